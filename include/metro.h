@@ -218,6 +218,90 @@ int moe_grouped_ffn_static_ws(const void* x, const int32_t* perm_pair, const int
 int moe_unpermute(const void* y_perm, const int32_t* pair_row, const float* topk_w, int T, int k, int H,
                   int dtype, void* out, void* stream);
 
+/*
+ * moe_permute_rows / moe_permute_rows_backward -- the tokens' rows sorted by expert, and the gradient of that:
+ *     x_perm[pair_row[t,j]] = x[t]                          (pairs on this rank)
+ *     dx[t] = sum over j ascending of dx_perm[pair_row[t,j]]    (pairs on this rank), accumulated in fp32; zeros where there is none
+ * Rows of x_perm that no pair names (those past n_pairs) are left as they were.  pair_row as in moe_unpermute; no row is named twice.
+ *
+ *   x, dx [T,H] dtype, pair_row [T,k] int32, x_perm, dx_perm [T*k,H] dtype.
+ */
+int moe_permute_rows(const void* x, const int32_t* pair_row, int T, int k, int H, int dtype, void* x_perm, void* stream);
+int moe_permute_rows_backward(const void* dx_perm, const int32_t* pair_row, int T, int k, int H, int dtype, void* dx, void* stream);
+
+/*
+ * moe_unpermute_backward -- the gradient of moe_unpermute.  For every pair of this rank, r = pair_row[t,j]:
+ *     dy_perm[r] = topk_w[t,j] * dout[t]
+ *     dtopk_w[t,j] = sum over H of dout[t] * y_perm[r], products and sums in fp32 in a fixed order; 0 for pairs of other ranks
+ * Rows of dy_perm that no pair names are left as they were; no row is named twice.
+ *
+ *   dout [T,H] dtype, y_perm, dy_perm [T*k,H] dtype, pair_row [T,k] int32, topk_w, dtopk_w [T,k] float32.
+ */
+int moe_unpermute_backward(const void* dout, const void* y_perm, const int32_t* pair_row, const float* topk_w, int T, int k, int H,
+                           int dtype, void* dy_perm, float* dtopk_w, void* stream);
+
+/*
+ * 8-bit experts.  Values are OCP e4m3 (1 byte; largest 448), with one fp32 scale for each block of 128: a value stands for
+ * byte * scale.  Activations have a scale for each 128 consecutive values of a row, scale [rows, ceil(K/128)]; a weight matrix one for
+ * each 128 rows x 128 columns, scale [ceil(rows/128), ceil(K/128)].  The last block of a row or matrix may be short.
+ * e4m3 rows are `ld` bytes apart, ld >= K, a multiple of 16 and at most 2^28, and start 16-byte aligned; the bytes from K up to the next multiple of
+ * 16 are read (their values do not matter), so they must be there, behind the last row too.
+ *
+ * moe_quantize_fp8 -- rows of activations (or of a gradient).  With m = max(largest magnitude of a block, 1e-30):
+ *     scale = m / 448        q = the e4m3 value nearest to x * (448 / m), ties to even        (each operation rounded to fp32)
+ * A block that holds a NaN gets scale NaN and NaNs; one that holds an infinity scale infinity, NaN in its place and zeros elsewhere.
+ *
+ *   x      [R,K]  dtype    rows ldx >= K elements apart
+ *   n_rows [1]    int32    rows to convert, read on the device (clamped to [0, R]); NULL = R.  Rows past it are left as they were
+ *   q      [R,K]  e4m3     out, rows ldq bytes apart (bytes past K are not written)
+ *   scale  [R, ceil(K/128)] float32 out
+ */
+int moe_quantize_fp8(const void* x, int ldx, int R, int K, int dtype, const int32_t* n_rows, void* q, int ldq, float* scale,
+                     void* stream);
+
+/*
+ * moe_quantize_weights_fp8 -- the same for `slots` matrices [rows, K], in blocks of 128 x 128.  For w13 as moe_grouped_ffn_fp8 reads it,
+ * pass the gate and up halves as matrices of their own: slots = 2*spr, rows = I.
+ *
+ *   w [slots,rows,K] dtype, rows ldw elements and slots rows*ldw elements apart; q [slots,rows,K] e4m3 out, likewise with ldq bytes;
+ *   scale [slots, ceil(rows/128), ceil(K/128)] float32 out.       Limit: fewer than 2^24 blocks.
+ */
+int moe_quantize_weights_fp8(const void* w, int ldw, int slots, int rows, int K, int dtype, void* q, int ldq, float* scale, void* stream);
+
+/*
+ * moe_grouped_mm_fp8 -- rows sorted by group (expert) times the weights of their group.  For row r of group l, with blocks b of K:
+ *     y[r][n] = sum over b of xs[r][b] * ws[l][n/128][b] * (sum over k in b of x[r][k] * w[l][n][k])
+ * products and sums in fp32, in a fixed order.  Only groups with at least one row are touched.  The gradient of x is the same call
+ * with transposed weights and scales on quantized rows of dy.
+ *
+ *   x      e4m3, xs float32     perm_pair NULL: [T*k,K], row r itself;  else [T,K], row r is that of token perm_pair[r] / k
+ *   group_offsets [groups+1] int32   rows of group l are [group_offsets[l], group_offsets[l+1])
+ *   w      [groups,N,K] e4m3    rows ldw bytes apart, groups N*ldw;   ws [groups, ceil(N/128), ceil(K/128)] float32
+ *   y      [T*k,N] dtype   out; rows past the last group are left as they were.  16-byte aligned
+ * Limits: groups <= 64, K, N <= 2^20, T*k < 2^24.
+ */
+int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const int32_t* perm_pair, const int32_t* group_offsets, int T, int k,
+                       int groups, int K, int N, const void* w, int ldw, const float* ws, int dtype, void* y, void* stream);
+
+/*
+ * moe_grouped_ffn_fp8 -- moe_grouped_ffn on 8-bit experts.  For row r of local slot l, token t = perm_pair[r] / k:
+ *     gate, up = x[t] . w13[l]^T          (as in moe_grouped_mm_fp8)
+ *     act = silu(gate) * up in fp32, then to e4m3 with a scale for each 128 as by moe_quantize_fp8
+ *     y_perm[r] = act . w2[l]^T
+ *
+ *   x      [T,H] e4m3, xs [T, ceil(H/128)] float32
+ *   w13    [spr,2I,H] e4m3   gate rows, then up rows; s13 [spr, 2*ceil(I/128), ceil(H/128)]: the blocks of up start at its first row
+ *   w2     [spr,H,I] e4m3    s2 [spr, ceil(H/128), ceil(I/128)]
+ *   y_perm [T*k,H] dtype     out: rows 0..n_pairs-1 are written.  16-byte aligned
+ *   ws     workspace of moe_grouped_ffn_fp8_workspace_bytes(); 256-byte aligned.  The figure for T tokens is enough for every smaller batch
+ * Weight pitches: as for moe_grouped_ffn, pad rows whose length is a multiple of 4096 bytes.
+ * Limits: spr <= 64, H, I <= 2^20, T*k < 2^24.
+ */
+size_t moe_grouped_ffn_fp8_workspace_bytes(int T, int k, int spr, int H, int I);
+int moe_grouped_ffn_fp8(const void* x, int ldx, const float* xs, const int32_t* perm_pair, const int32_t* group_offsets, int T, int k,
+                        int spr, int H, int I, const void* w13, int ldw13, const float* s13, const void* w2, int ldw2, const float* s2,
+                        int dtype, void* y_perm, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,7 +33,9 @@ EXPORTS = ("metro_status_string", "metro_route", "metro_route_token_balanced", "
            "moe_grouped_ffn_workspace_bytes", "moe_grouped_ffn", "moe_grouped_ffn_gate_up",
            "moe_grouped_ffn_down", "moe_unpermute", "moe_gate_topk_workspace_bytes", "moe_gate_topk",
            "moe_grouped_ffn_static_ws_bytes", "moe_grouped_ffn_static_ws", "metro_route_permute",
-           "metro_route_token_balanced_permute")
+           "metro_route_token_balanced_permute", "moe_permute_rows", "moe_permute_rows_backward", "moe_unpermute_backward",
+           "moe_quantize_fp8", "moe_quantize_weights_fp8", "moe_grouped_mm_fp8", "moe_grouped_ffn_fp8_workspace_bytes",
+           "moe_grouped_ffn_fp8")
 
 
 class MetroError(RuntimeError):
@@ -82,6 +84,22 @@ def load() -> ctypes.CDLL:
         lib.moe_gate_topk_workspace_bytes.argtypes = [ci, ci, ci, ci]
         lib.moe_gate_topk.restype = ci
         lib.moe_gate_topk.argtypes = [vp, vp, ci, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp]
+        lib.moe_permute_rows.restype = ci
+        lib.moe_permute_rows.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp]
+        lib.moe_permute_rows_backward.restype = ci
+        lib.moe_permute_rows_backward.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp]
+        lib.moe_unpermute_backward.restype = ci
+        lib.moe_unpermute_backward.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp]
+        lib.moe_quantize_fp8.restype = ci
+        lib.moe_quantize_fp8.argtypes = [vp, ci, ci, ci, ci, vp, vp, ci, vp, vp]
+        lib.moe_quantize_weights_fp8.restype = ci
+        lib.moe_quantize_weights_fp8.argtypes = [vp, ci, ci, ci, ci, ci, vp, ci, vp, vp]
+        lib.moe_grouped_mm_fp8.restype = ci
+        lib.moe_grouped_mm_fp8.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, ci, ci, vp, ci, vp, ci, vp, vp]
+        lib.moe_grouped_ffn_fp8_workspace_bytes.restype = sz
+        lib.moe_grouped_ffn_fp8_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+        lib.moe_grouped_ffn_fp8.restype = ci
+        lib.moe_grouped_ffn_fp8.argtypes = [vp, ci, vp, vp, vp, ci, ci, ci, ci, ci, vp, ci, vp, vp, ci, vp, ci, vp, vp, sz, vp]
         _fn.update({name: ctypes.cast(getattr(lib, name), vp).value for name in EXPORTS})
         _native = importlib.import_module("._call", __package__)
         _lib = lib
@@ -374,3 +392,237 @@ def moe_gate_topk(x: torch.Tensor, w_gate: torch.Tensor, k: int, out: Optional[d
                                 _dev(out["expert_count"], torch.int32, "expert_count"),
                                 _dev(ws, torch.uint8, "ws"), ws.numel(), _stream()))
     return out
+
+
+# ------------------------------------------------------------------------------------------ sorted rows and gradients
+def _on_current_device(**tensors) -> None:
+    """A launch goes to the current device's stream, so that is where its tensors have to be."""
+    on_gpu = {name: t.device for name, t in tensors.items() if t is not None and t.is_cuda}
+    here = torch.cuda.current_device() if on_gpu else None
+    for name, device in on_gpu.items():
+        if device.index != here:
+            raise ValueError(f"{name} is on {device}, the current device is cuda:{here}")
+
+
+def _shaped(t: torch.Tensor, shape, name: str) -> torch.Tensor:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def moe_permute_rows(x: torch.Tensor, pair_row: torch.Tensor, x_perm: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x [T,H] (bf16 or f32), pair_row [T,k] int32 -> x_perm [T*k,H]: row pair_row[t,j] is x[t].  Rows that no pair names (those past
+    n_pairs) are left as they were."""
+    load()
+    if x_perm is not None:
+        status = _native.rows(_fn["moe_permute_rows"], 0, x, pair_row, x_perm)
+        if status != _UNUSUAL:
+            _check(status)
+            return x_perm
+    T, H = x.shape
+    k = _shaped(pair_row, (T, pair_row.shape[-1]), "pair_row").shape[1]
+    code = _dtype_code(x)
+    if x_perm is None:
+        x_perm = torch.empty((T * k, H), dtype=x.dtype, device=x.device)
+    _on_current_device(x=x, pair_row=pair_row, x_perm=x_perm)
+    _check(load().moe_permute_rows(_dev(x, x.dtype, "x"), _dev(pair_row, torch.int32, "pair_row"), T, k, H, code,
+                                   _dev(_shaped(x_perm, (T * k, H), "x_perm"), x.dtype, "x_perm"), _stream()))
+    return x_perm
+
+
+def moe_permute_rows_backward(dx_perm: torch.Tensor, pair_row: torch.Tensor, dx: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of moe_permute_rows: dx_perm [T*k,H], pair_row [T,k] -> dx [T,H], the sum of a token's rows."""
+    load()
+    if dx is not None:
+        status = _native.rows(_fn["moe_permute_rows_backward"], 1, dx_perm, pair_row, dx)
+        if status != _UNUSUAL:
+            _check(status)
+            return dx
+    T, k = pair_row.shape
+    H = dx_perm.shape[-1]
+    _shaped(dx_perm, (T * k, H), "dx_perm")
+    code = _dtype_code(dx_perm)
+    if dx is None:
+        dx = torch.empty((T, H), dtype=dx_perm.dtype, device=dx_perm.device)
+    _on_current_device(dx_perm=dx_perm, pair_row=pair_row, dx=dx)
+    _check(load().moe_permute_rows_backward(_dev(dx_perm, dx_perm.dtype, "dx_perm"), _dev(pair_row, torch.int32, "pair_row"), T, k, H,
+                                            code, _dev(_shaped(dx, (T, H), "dx"), dx_perm.dtype, "dx"), _stream()))
+    return dx
+
+
+def moe_unpermute_backward(dout: torch.Tensor, y_perm: torch.Tensor, pair_row: torch.Tensor, topk_w: torch.Tensor,
+                           dy_perm: Optional[torch.Tensor] = None, dtopk_w: Optional[torch.Tensor] = None):
+    """The gradient of moe_unpermute: dout [T,H], y_perm [T*k,H], pair_row [T,k], topk_w [T,k] float32 -> (dy_perm [T*k,H], of which
+    rows that no pair names are left as they were; dtopk_w [T,k] float32, 0 for pairs of other ranks)."""
+    load()
+    if dy_perm is not None and dtopk_w is not None:
+        status = _native.unpermute_backward(_fn["moe_unpermute_backward"], dout, y_perm, pair_row, topk_w, dy_perm, dtopk_w)
+        if status != _UNUSUAL:
+            _check(status)
+            return dy_perm, dtopk_w
+    T, H = dout.shape
+    k = _shaped(pair_row, (T, pair_row.shape[-1]), "pair_row").shape[1]
+    code = _dtype_code(dout)
+    if dy_perm is None:
+        dy_perm = torch.empty((T * k, H), dtype=dout.dtype, device=dout.device)
+    if dtopk_w is None:
+        dtopk_w = torch.empty((T, k), dtype=torch.float32, device=dout.device)
+    _on_current_device(dout=dout, y_perm=y_perm, pair_row=pair_row, topk_w=topk_w, dy_perm=dy_perm, dtopk_w=dtopk_w)
+    _check(load().moe_unpermute_backward(
+        _dev(dout, dout.dtype, "dout"), _dev(_shaped(y_perm, (T * k, H), "y_perm"), dout.dtype, "y_perm"),
+        _dev(pair_row, torch.int32, "pair_row"), _dev(_shaped(topk_w, (T, k), "topk_w"), torch.float32, "topk_w"), T, k, H, code,
+        _dev(_shaped(dy_perm, (T * k, H), "dy_perm"), dout.dtype, "dy_perm"),
+        _dev(_shaped(dtopk_w, (T, k), "dtopk_w"), torch.float32, "dtopk_w"), _stream()))
+    return dy_perm, dtopk_w
+
+
+# ------------------------------------------------------------------------------------------ 8-bit experts
+FP8 = torch.float8_e4m3fn
+BLOCK = 128                 # values of a row that share a scale; rows and columns of a weight block
+
+
+def _blocks(n: int) -> int:
+    return (n + BLOCK - 1) // BLOCK
+
+
+def _fp8_matrix(t: torch.Tensor, name: str):
+    """e4m3 [.., rows, K]: K contiguous, rows `ld` bytes apart (a multiple of 16), matrices rows*ld apart, and the last row's bytes up
+    to a multiple of 16 inside the storage.  Returns (pointer, ld)."""
+    if not (t.is_cuda and t.dtype == FP8 and t.dim() in (2, 3)):
+        raise TypeError(f"{name}: expected a {FP8} device tensor of rows, got {t.dtype} on {t.device}")
+    lead = t.shape[0] if t.dim() == 3 else 1
+    rows, K = t.shape[-2:]
+    k16 = (K + 15) // 16 * 16
+    one = rows <= 1
+    ld = t.stride(-2) if not one else t.stride(0) if t.dim() == 3 and lead > 1 else k16
+    if (K > 1 and t.stride(-1) != 1) or ld < K or ld % 16 or (t.dim() == 3 and lead > 1 and t.stride(0) != rows * ld):
+        raise TypeError(f"{name}: rows must be K-contiguous, a multiple of 16 bytes apart (strides {t.stride()})")
+    if t.numel() and t.storage_offset() + (lead * rows - 1) * ld + k16 > t.untyped_storage().nbytes():
+        raise ValueError(f"{name}: the last row must be readable up to a multiple of 16 bytes")
+    return t.data_ptr(), ld
+
+
+def quantize_buffers(R: int, K: int, device) -> Dict[str, torch.Tensor]:
+    """Output buffers of moe_quantize_fp8: rows padded to a multiple of 16 bytes."""
+    q = torch.empty((R, (K + 15) // 16 * 16), dtype=torch.uint8, device=device).view(FP8)
+    return dict(q=q[:, :K], scale=torch.empty((R, _blocks(K)), dtype=torch.float32, device=device))
+
+
+def quantize_weights_buffers(slots: int, rows: int, K: int, device) -> Dict[str, torch.Tensor]:
+    """Output buffers of moe_quantize_weights_fp8: rows a multiple of 16 bytes and not of 4096 bytes apart."""
+    pitch = K + BLOCK if K % 4096 == 0 else (K + 15) // 16 * 16
+    q = torch.empty((slots, rows, pitch), dtype=torch.uint8, device=device).view(FP8)
+    return dict(q=q[:, :, :K], scale=torch.empty((slots, _blocks(rows), _blocks(K)), dtype=torch.float32, device=device))
+
+
+def moe_quantize_fp8(x: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
+                     out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """x [R,K] (bf16 or f32; rows may be strided) -> dict(q [R,K] e4m3, scale [R,ceil(K/128)] float32).  n_rows: int32 device tensor of
+    one element, the rows to convert (those past it are left as they were)."""
+    load()
+    if out is not None:
+        status = _native.quantize(_fn["moe_quantize_fp8"], x, n_rows, out)
+        if status != _UNUSUAL:
+            _check(status)
+            return out
+    R, K = x.shape
+    code = _dtype_code(x)
+    if out is None:
+        out = quantize_buffers(R, K, x.device)
+    _on_current_device(x=x, n_rows=n_rows, q=out["q"], scale=out["scale"])
+    if not x.is_cuda or (K > 1 and x.stride(1) != 1) or (R > 1 and x.stride(0) < K):
+        raise TypeError(f"x: expected a device tensor with contiguous rows, got strides {x.stride()} on {x.device}")
+    q, ldq = _fp8_matrix(_shaped(out["q"], (R, K), "q"), "q")
+    nr = None if n_rows is None else _dev(_shaped(n_rows, (1,), "n_rows"), torch.int32, "n_rows")
+    _check(load().moe_quantize_fp8(x.data_ptr(), x.stride(0) if R > 1 else K, R, K, code, nr, q, ldq,
+                                   _dev(_shaped(out["scale"], (R, _blocks(K)), "scale"), torch.float32, "scale"), _stream()))
+    return out
+
+
+def moe_quantize_weights_fp8(w: torch.Tensor, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """w [slots,rows,K] (bf16 or f32; rows may be padded) -> dict(q [slots,rows,K] e4m3, scale [slots,ceil(rows/128),ceil(K/128)]
+    float32).  For w13 [spr,2I,H], whose gate and up halves have blocks of their own, pass w13.view(2*spr, I, H)."""
+    S, rows, K = w.shape
+    code = _dtype_code(w)
+    if out is None:
+        out = quantize_weights_buffers(S, rows, K, w.device)
+    _on_current_device(w=w, q=out["q"], scale=out["scale"])
+    p, ld = _weights(w, w.dtype, "w")
+    q, ldq = _fp8_matrix(_shaped(out["q"], (S, rows, K), "q"), "q")
+    _check(load().moe_quantize_weights_fp8(p, ld, S, rows, K, code, q, ldq,
+                                           _dev(_shaped(out["scale"], (S, _blocks(rows), _blocks(K)), "scale"), torch.float32, "scale"),
+                                           _stream()))
+    return out
+
+
+def moe_grouped_mm_fp8(x: torch.Tensor, xs: torch.Tensor, group_offsets: torch.Tensor, w: torch.Tensor, ws: torch.Tensor,
+                       y: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                       perm_pair: Optional[torch.Tensor] = None, k: int = 1) -> torch.Tensor:
+    """Rows sorted by group times their group's weights: x [R,K] e4m3, xs [R,ceil(K/128)], w [groups,N,K] e4m3,
+    ws [groups,ceil(N/128),ceil(K/128)] -> y [R,N] (bf16 or f32, `dtype` where y is not given; rows past the last group are left as they
+    were).  With perm_pair, x holds tokens [T,K], row r is that of token perm_pair[r] // k, and y is [T*k,N]."""
+    load()
+    if y is not None:
+        status = _native.mm_fp8(_fn["moe_grouped_mm_fp8"], x, xs, group_offsets, w, ws, y, perm_pair, k)
+        if status != _UNUSUAL:
+            _check(status)
+            return y
+    T, K = x.shape
+    groups, N, _ = w.shape
+    if perm_pair is None and k != 1:
+        raise ValueError("k without perm_pair")
+    if k < 1 or (perm_pair is not None and perm_pair.numel() < T * k):
+        raise ValueError("perm_pair must hold T*k entries")
+    if y is None:
+        y = torch.empty((T * k, N), dtype=dtype, device=x.device)
+    _on_current_device(x=x, xs=xs, group_offsets=group_offsets, w=w, ws=ws, y=y, perm_pair=perm_pair)
+    px, ldx = _fp8_matrix(x, "x")
+    pw, ldw = _fp8_matrix(_shaped(w, (groups, N, K), "w"), "w")
+    _check(load().moe_grouped_mm_fp8(
+        px, ldx, _dev(_shaped(xs, (T, _blocks(K)), "xs"), torch.float32, "xs"),
+        None if perm_pair is None else _dev(perm_pair, torch.int32, "perm_pair"),
+        _dev(_shaped(group_offsets, (groups + 1,), "group_offsets"), torch.int32, "group_offsets"), T, k, groups, K, N, pw, ldw,
+        _dev(_shaped(ws, (groups, _blocks(N), _blocks(K)), "ws"), torch.float32, "ws"), _dtype_code(y),
+        _dev(_shaped(y, (T * k, N), "y"), y.dtype, "y"), _stream()))
+    return y
+
+
+def moe_grouped_ffn_fp8_workspace_bytes(T: int, k: int, spr: int, H: int, I: int) -> int:
+    return int(load().moe_grouped_ffn_fp8_workspace_bytes(T, k, spr, H, I))
+
+
+def moe_grouped_ffn_fp8(x: torch.Tensor, xs: torch.Tensor, perm_pair: torch.Tensor, group_offsets: torch.Tensor, k: int,
+                        w13: torch.Tensor, s13: torch.Tensor, w2: torch.Tensor, s2: torch.Tensor,
+                        y_perm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                        dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """moe_grouped_ffn on 8-bit experts: x [T,H] e4m3 with xs [T,ceil(H/128)], w13 [spr,2I,H] e4m3 with s13 [spr,2*ceil(I/128),
+    ceil(H/128)], w2 [spr,H,I] e4m3 with s2 [spr,ceil(H/128),ceil(I/128)] -> y_perm [T*k,H] (bf16 or f32, `dtype` where it is not given;
+    rows < n_pairs written)."""
+    load()
+    if y_perm is not None and ws is not None:
+        status = _native.ffn_fp8(_fn["moe_grouped_ffn_fp8"], x, xs, perm_pair, group_offsets, k, w13, s13, w2, s2, y_perm, ws)
+        if status != _UNUSUAL:
+            _check(status)
+            return y_perm
+    T, H = x.shape
+    spr, two_i, _ = w13.shape
+    I = two_i // 2
+    _shaped(w13, (spr, 2 * I, H), "w13")
+    _shaped(w2, (spr, H, I), "w2")
+    if perm_pair.numel() < T * k:
+        raise ValueError("perm_pair must hold T*k entries")
+    if y_perm is None:
+        y_perm = torch.empty((T * k, H), dtype=dtype, device=x.device)
+    if ws is None:
+        ws = torch.empty((moe_grouped_ffn_fp8_workspace_bytes(T, k, spr, H, I),), dtype=torch.uint8, device=x.device)
+    _on_current_device(x=x, xs=xs, perm_pair=perm_pair, group_offsets=group_offsets, w13=w13, s13=s13, w2=w2, s2=s2, y_perm=y_perm, ws=ws)
+    px, ldx = _fp8_matrix(x, "x")
+    p13, ld13 = _fp8_matrix(w13, "w13")
+    p2, ld2 = _fp8_matrix(w2, "w2")
+    _check(load().moe_grouped_ffn_fp8(
+        px, ldx, _dev(_shaped(xs, (T, _blocks(H)), "xs"), torch.float32, "xs"), _dev(perm_pair, torch.int32, "perm_pair"),
+        _dev(_shaped(group_offsets, (spr + 1,), "group_offsets"), torch.int32, "group_offsets"), T, k, spr, H, I,
+        p13, ld13, _dev(_shaped(s13, (spr, 2 * _blocks(I), _blocks(H)), "s13"), torch.float32, "s13"),
+        p2, ld2, _dev(_shaped(s2, (spr, _blocks(H), _blocks(I)), "s2"), torch.float32, "s2"), _dtype_code(y_perm),
+        _dev(_shaped(y_perm, (T * k, H), "y_perm"), y_perm.dtype, "y_perm"), _dev(ws, torch.uint8, "ws"), ws.numel(), _stream()))
+    return y_perm

@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 
 #include "metro.h"
 
@@ -229,6 +230,144 @@ PyObject* gate_topk(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return call<decltype(&moe_gate_topk)>(fn, px, Ptr{const_cast<void*>(w->const_data_ptr())}, (int)ldw, (int)T, (int)H, (int)N, k, code, pnv, ids, tw, cnt, pws, (size_t)ws->numel(), stream);
 }
 
+// All on the device of the current stream; the calls below refuse anything else.
+bool on_current_device(Args& a, std::initializer_list<const at::Tensor*> all) {
+    if (!a.ok) return false;
+    PyObject* device = PyObject_CallNoArgs(get_device);
+    const long here = device ? PyLong_AsLong(device) : -1;
+    Py_XDECREF(device);
+    if (PyErr_Occurred()) return PyErr_Clear(), a.ok = false;
+    for (const at::Tensor* t : all)
+        if (t->get_device() != here) a.ok = false;
+    return a.ok;
+}
+
+bool is(const at::Tensor* t, int64_t rows, int64_t cols) { return t->dim() == 2 && t->size(0) == rows && t->size(1) == cols; }
+bool is(const at::Tensor* t, int64_t n, int64_t rows, int64_t cols) {
+    return t->dim() == 3 && t->size(0) == n && t->size(1) == rows && t->size(2) == cols;
+}
+int64_t blocks(int64_t n) { return (n + 127) / 128; }
+
+// A tensor or None (null, with a.ok as it was).
+const at::Tensor* optional_tensor(Args& a) {
+    PyObject* o = a.next();
+    return o && o != Py_None ? a.as_tensor(o) : nullptr;
+}
+
+// e4m3 rows (of the last two dimensions), K contiguous, `ld` bytes apart, matrices rows * ld apart, the last row's bytes up to a
+// multiple of 16 inside the storage.
+Ptr fp8_rows(Args& a, const at::Tensor* t, int& ld, bool written = false) {
+    const int64_t d = t->dim();
+    if (!a.ok || t->scalar_type() != at::kFloat8_e4m3fn || d < 2 || d > 3 || t->numel() == 0) return a.ok = false, Ptr{};
+    const int64_t lead = d == 3 ? t->size(0) : 1, rows = t->size(d - 2), K = t->size(d - 1), k16 = (K + 15) / 16 * 16;
+    const int64_t pitch = rows > 1 ? t->stride(d - 2) : lead > 1 ? t->stride(0) : k16;
+    if ((K > 1 && t->stride(d - 1) != 1) || pitch < K || pitch % 16 || !fits(pitch) || (lead > 1 && t->stride(0) != rows * pitch) ||
+        t->storage_offset() + (lead * rows - 1) * pitch + k16 > (int64_t)t->storage().nbytes())
+        return a.ok = false, Ptr{};
+    ld = (int)pitch;
+    return Ptr{written ? t->mutable_data_ptr() : const_cast<void*>(t->const_data_ptr())};
+}
+
+// rows(fn, gather, src, pair_row, dst): gather 0: src [T,H], dst [T*k,H]; 1: the other way round
+PyObject* rows(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a{v, n};
+    void* fn = a.address();
+    const int gather = a.integer();
+    const at::Tensor *src = a.tensor(), *row = a.tensor(), *dst = a.tensor();
+    if (!a.ok || row->dim() != 2 || src->dim() != 2) return unusual();
+    const int64_t T = row->size(0), k = row->size(1), H = src->size(1);
+    if (!fits(T) || !fits(k) || !fits(H) || !is(src, gather ? T * k : T, H) || !is(dst, gather ? T : T * k, H)) return unusual();
+    const int code = dtype_code(a, src);
+    const Ptr ps = a.in(src, src->scalar_type()), pr = a.in(row), pd = a.out(dst, src->scalar_type());
+    void* stream = current_stream(a);
+    if (!on_current_device(a, {src, row, dst})) return unusual();
+    if (gather) return call<decltype(&moe_permute_rows_backward)>(fn, ps, pr, (int)T, (int)k, (int)H, code, pd, stream);
+    return call<decltype(&moe_permute_rows)>(fn, ps, pr, (int)T, (int)k, (int)H, code, pd, stream);
+}
+
+// unpermute_backward(fn, dout, y_perm, pair_row, topk_w, dy_perm, dtopk_w)
+PyObject* unpermute_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a{v, n};
+    void* fn = a.address();
+    const at::Tensor *g = a.tensor(), *y = a.tensor(), *row = a.tensor(), *w = a.tensor(), *dy = a.tensor(), *dw = a.tensor();
+    if (!a.ok || row->dim() != 2 || g->dim() != 2) return unusual();
+    const int64_t T = row->size(0), k = row->size(1), H = g->size(1);
+    if (!fits(T) || !fits(k) || !fits(H) || !is(g, T, H) || !is(y, T * k, H) || !is(w, T, k) || !is(dy, T * k, H) || !is(dw, T, k))
+        return unusual();
+    const int code = dtype_code(a, g);
+    const at::ScalarType type = g->scalar_type();
+    const Ptr pg = a.in(g, type), py = a.in(y, type), pr = a.in(row), pw = a.in(w, at::kFloat), pdy = a.out(dy, type),
+              pdw = a.out(dw, at::kFloat);
+    void* stream = current_stream(a);
+    if (!on_current_device(a, {g, y, row, w, dy, dw})) return unusual();
+    return call<decltype(&moe_unpermute_backward)>(fn, pg, py, pr, pw, (int)T, (int)k, (int)H, code, pdy, pdw, stream);
+}
+
+// quantize(fn, x, n_rows or None, out)
+PyObject* quantize(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a{v, n};
+    void* fn = a.address();
+    const at::Tensor *x = a.tensor(), *nr = optional_tensor(a);
+    PyObject* out = a.next();
+    const at::Tensor *q = a.field(out, "q"), *scale = a.field(out, "scale");
+    if (!a.ok || x->dim() != 2 || x->numel() == 0) return unusual();
+    const int64_t R = x->size(0), K = x->size(1), ld = R > 1 ? x->stride(0) : K;
+    if (!fits(R) || !fits(K) || !fits(ld) || ld < K || (K > 1 && x->stride(1) != 1) || !is(q, R, K) || !is(scale, R, blocks(K)) ||
+        (nr && (nr->dim() != 1 || nr->size(0) != 1)))
+        return unusual();
+    const int code = dtype_code(a, x);
+    int ldq = 0;
+    const Ptr pq = fp8_rows(a, q, ldq, true), ps = a.out(scale, at::kFloat), pn = nr ? a.in(nr) : Ptr{};
+    void* stream = current_stream(a);
+    if (!on_current_device(a, {x, nr ? nr : x, q, scale})) return unusual();
+    return call<decltype(&moe_quantize_fp8)>(fn, Ptr{const_cast<void*>(x->const_data_ptr())}, (int)ld, (int)R, (int)K, code, pn, pq, ldq, ps, stream);
+}
+
+// mm_fp8(fn, x, xs, group_offsets, w, ws, y, perm_pair or None, k)
+PyObject* mm_fp8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a{v, n};
+    void* fn = a.address();
+    const at::Tensor *x = a.tensor(), *xs = a.tensor(), *offsets = a.tensor(), *w = a.tensor(), *ws = a.tensor(), *y = a.tensor(),
+                     *perm = optional_tensor(a);
+    const int k = a.integer();
+    if (!a.ok || x->dim() != 2 || w->dim() != 3 || k < 1 || (!perm && k != 1)) return unusual();
+    const int64_t T = x->size(0), K = x->size(1), groups = w->size(0), N = w->size(1);
+    if (!fits(T) || !fits(K) || !fits(groups) || !fits(N) || w->size(2) != K || !is(xs, T, blocks(K)) || !is(ws, groups, blocks(N), blocks(K)) ||
+        !is(y, T * k, N) || offsets->dim() != 1 || offsets->size(0) != groups + 1 || (perm && perm->numel() < T * k))
+        return unusual();
+    const int code = dtype_code(a, y);
+    int ldx = 0, ldw = 0;
+    const Ptr px = fp8_rows(a, x, ldx), pw = fp8_rows(a, w, ldw), pxs = a.in(xs, at::kFloat), pws = a.in(ws, at::kFloat),
+              po = a.in(offsets), pp = perm ? a.in(perm) : Ptr{}, py = a.out(y, y->scalar_type());
+    void* stream = current_stream(a);
+    if (!on_current_device(a, {x, xs, offsets, w, ws, y, perm ? perm : x})) return unusual();
+    return call<decltype(&moe_grouped_mm_fp8)>(fn, px, ldx, pxs, pp, po, (int)T, k, (int)groups, (int)K, (int)N, pw, ldw, pws, code, py, stream);
+}
+
+// ffn_fp8(fn, x, xs, perm_pair, group_offsets, k, w13, s13, w2, s2, y_perm, ws)
+PyObject* ffn_fp8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a{v, n};
+    void* fn = a.address();
+    const at::Tensor *x = a.tensor(), *xs = a.tensor(), *perm = a.tensor(), *offsets = a.tensor();
+    const int k = a.integer();
+    const at::Tensor *w13 = a.tensor(), *s13 = a.tensor(), *w2 = a.tensor(), *s2 = a.tensor(), *y = a.tensor(), *ws = a.tensor();
+    if (!a.ok || x->dim() != 2 || w13->dim() != 3 || k < 1) return unusual();
+    const int64_t T = x->size(0), H = x->size(1), spr = w13->size(0), I = w13->size(1) / 2;
+    if (!fits(T) || !fits(H) || !fits(spr) || !fits(I) || !is(w13, spr, 2 * I, H) || !is(w2, spr, H, I) || !is(xs, T, blocks(H)) ||
+        !is(s13, spr, 2 * blocks(I), blocks(H)) || !is(s2, spr, blocks(H), blocks(I)) || !is(y, T * k, H) || perm->numel() < T * k ||
+        offsets->dim() != 1 || offsets->size(0) != spr + 1)
+        return unusual();
+    const int code = dtype_code(a, y);
+    int ldx = 0, ld13 = 0, ld2 = 0;
+    const Ptr px = fp8_rows(a, x, ldx), p13 = fp8_rows(a, w13, ld13), p2 = fp8_rows(a, w2, ld2), pxs = a.in(xs, at::kFloat),
+              ps13 = a.in(s13, at::kFloat), ps2 = a.in(s2, at::kFloat), pp = a.in(perm), po = a.in(offsets),
+              py = a.out(y, y->scalar_type()), pws = a.out(ws, at::kByte);
+    void* stream = current_stream(a);
+    if (!on_current_device(a, {x, xs, perm, offsets, w13, s13, w2, s2, y, ws})) return unusual();
+    return call<decltype(&moe_grouped_ffn_fp8)>(fn, px, ldx, pxs, pp, po, (int)T, k, (int)spr, (int)H, (int)I, p13, ld13, ps13, p2, ld2, ps2, code,
+                                                py, pws, (size_t)ws->numel(), stream);
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
     try {
@@ -240,7 +379,9 @@ PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
 
 #define METRO_CALL(f) {#f, (PyCFunction)(void (*)(void))guarded<f>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METRO_CALL(route),     METRO_CALL(route_permute), METRO_CALL(ffn),
-                         METRO_CALL(unpermute), METRO_CALL(gate_topk),     {nullptr, nullptr, 0, nullptr}};
+                         METRO_CALL(unpermute), METRO_CALL(gate_topk),     METRO_CALL(rows),
+                         METRO_CALL(unpermute_backward), METRO_CALL(quantize), METRO_CALL(mm_fp8),
+                         METRO_CALL(ffn_fp8),   {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,113 @@
+// moe_grouped_mm_fp8 and moe_grouped_ffn_fp8: rows sorted by expert times their expert's e4m3 weights, rows and weights with an fp32
+// scale for each block of 128 (fp8_common.h).
+//
+// Decode is bound by the weights' bytes, half of bf16's: every activated weight row is streamed once per tile (fp8_split.h).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "fp8_common.h"
+#include "fp8_split.h"
+#include "metro.h"
+
+namespace metro {
+namespace {
+
+constexpr int kNarrowRows32 = 32;
+constexpr int kNarrowGrid = 1536;           // three rounds of the 512 resident workgroups, the rest in turns
+
+template <bool kGateUp, bool kQuantX, typename OT, bool kRagged>
+__global__ __launch_bounds__(kFp8Threads, 2) void fp8_narrow_kernel(Fp8Args a, int64_t n_items) {
+    __shared__ __attribute__((aligned(16))) char mem[65536];
+    __shared__ float scale[4 * 64];
+    const Fp8Lds lds{mem, scale};
+    for (int64_t id = blockIdx.x; id < n_items; id += gridDim.x) {
+        const Item it = locate_in_order(a.group_offsets, a.groups, a.T * a.k, kNarrowRows32, a.ntn, id);
+        if (!it.valid) return;                                       // uniform; items are consecutive
+        if (it.tile.rows <= 16) fp8_tile<kGateUp, kQuantX, OT, 1, 2, kRagged>(a, it.tile, lds);
+        else fp8_tile<kGateUp, kQuantX, OT, 2, 1, kRagged>(a, it.tile, lds);
+        __syncthreads();                                             // the next item's sums reuse the LDS
+    }
+}
+
+inline int launched() { return hipGetLastError() == hipSuccess ? METRO_OK : METRO_ERR_HIP; }
+
+// dtype: of dst
+template <bool kGateUp, bool kQuantX>
+int launch(Fp8Args a, int dtype, hipStream_t st) {
+    const int cols = kFp8Blocks * (kGateUp ? 8 : 16);
+    a.ntn = (a.n_out + cols - 1) / cols;
+    const int64_t n_items = (int64_t)max_tiles(a.T * a.k, a.groups, kNarrowRows32) * a.ntn;
+    const uint32_t grid = (uint32_t)std::min<int64_t>(n_items, kNarrowGrid);
+    const bool whole = a.K % kBlock == 0 && a.n_out % kBlock == 0;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kFp8Threads), 0, st, a, n_items); };
+    if (kGateUp || dtype == METRO_DTYPE_F32) {
+        if (whole) go(fp8_narrow_kernel<kGateUp, kQuantX, float, false>);
+        else go(fp8_narrow_kernel<kGateUp, kQuantX, float, true>);
+    } else if constexpr (!kGateUp) {
+        if (whole) go(fp8_narrow_kernel<kGateUp, kQuantX, __bf16, false>);
+        else go(fp8_narrow_kernel<kGateUp, kQuantX, __bf16, true>);
+    }
+    return launched();
+}
+
+constexpr int kMaxSide = 1 << 20;           // K, columns
+constexpr int kMaxPitch = 1 << 28;          // eight rows are addressed in 32 bits
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+int check_sizes(const int32_t* group_offsets, int T, int k, int groups, int H, int I, int dtype) {
+    if (T < 0 || k < 1 || groups < 1 || H < 1 || I < 1 || !group_offsets) return METRO_ERR_INVALID_ARG;
+    if (dtype != METRO_DTYPE_BF16 && dtype != METRO_DTYPE_F32) return METRO_ERR_UNSUPPORTED;
+    if (groups > kMaxSpr || (int64_t)T * k >= (1 << 24) || H > kMaxSide || I > kMaxSide) return METRO_ERR_UNSUPPORTED;
+    return METRO_OK;
+}
+
+int check_matrix(const void* p, int ld, int K, const float* scale) {
+    return !p || !scale || misaligned(p) || ld < K || ld % 16 != 0 || ld > kMaxPitch ? METRO_ERR_INVALID_ARG : METRO_OK;
+}
+
+inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+inline size_t act_bytes(int T, int k, int I) { return align256((size_t)T * k * up16(I) * 4); }
+
+}  // namespace
+}  // namespace metro
+
+extern "C" int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const int32_t* perm_pair, const int32_t* group_offsets, int T,
+                                  int k, int groups, int K, int N, const void* w, int ldw, const float* ws, int dtype, void* y,
+                                  void* stream) {
+    using namespace metro;
+    const int rc = check_sizes(group_offsets, T, k, groups, K, N, dtype);
+    if (rc != METRO_OK) return rc;
+    if (T == 0) return METRO_OK;
+    if (check_matrix(x, ldx, K, xs) != METRO_OK || check_matrix(w, ldw, K, ws) != METRO_OK || !y || misaligned(y)) return METRO_ERR_INVALID_ARG;
+    const Fp8Args a{x, xs, perm_pair, group_offsets, (const uint8_t*)w, ws, y, ldx, T, k, groups, K, N, ldw, N, 0};
+    return launch<false, false>(a, dtype, (hipStream_t)stream);
+}
+
+extern "C" size_t moe_grouped_ffn_fp8_workspace_bytes(int T, int k, int spr, int H, int I) {
+    using namespace metro;
+    if (T < 0 || k < 1 || spr < 1 || H < 1 || I < 1) return 0;
+    return act_bytes(T, k, I) + 256;
+}
+
+extern "C" int moe_grouped_ffn_fp8(const void* x, int ldx, const float* xs, const int32_t* perm_pair, const int32_t* group_offsets, int T,
+                                   int k, int spr, int H, int I, const void* w13, int ldw13, const float* s13, const void* w2, int ldw2,
+                                   const float* s2, int dtype, void* y_perm, void* ws, size_t ws_bytes, void* stream) {
+    using namespace metro;
+    int rc = check_sizes(group_offsets, T, k, spr, H, I, dtype);
+    if (rc != METRO_OK) return rc;
+    if (T == 0) return METRO_OK;
+    if (check_matrix(x, ldx, H, xs) != METRO_OK || check_matrix(w13, ldw13, H, s13) != METRO_OK || check_matrix(w2, ldw2, I, s2) != METRO_OK ||
+        !perm_pair || !y_perm || misaligned(y_perm) || !ws || ((uintptr_t)ws & 255) != 0)
+        return METRO_ERR_INVALID_ARG;
+    if (ws_bytes < moe_grouped_ffn_fp8_workspace_bytes(T, k, spr, H, I)) return METRO_ERR_WORKSPACE;
+    const int ld_act = (int)up16(I);
+    const Fp8Args up{x, xs, perm_pair, group_offsets, (const uint8_t*)w13, s13, ws, ldx, T, k, spr, H, I, ldw13, ld_act, 0};
+    rc = launch<true, false>(up, METRO_DTYPE_F32, (hipStream_t)stream);
+    if (rc != METRO_OK) return rc;
+    const Fp8Args down{ws, nullptr, nullptr, group_offsets, (const uint8_t*)w2, s2, y_perm, ld_act, T, k, spr, I, H, ldw2, H, 0};
+    return launch<false, true>(down, dtype, (hipStream_t)stream);
+}

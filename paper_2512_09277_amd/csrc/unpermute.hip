@@ -1,25 +1,19 @@
 // moe_unpermute: one rank's share of the combine step -- a gather of the rows a token owns in
-// y_perm, weighted by the gating weights and summed in fp32 in ascending j.
+// y_perm, weighted by the gating weights and summed in fp32 in ascending j.  With all weights 1 it is the gradient of
+// moe_permute_rows (moe_permute_rows_backward).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
 
 #include "metro.h"
+#include "row_vec.h"
 
 namespace metro {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxThreads = 1024;
-
-__device__ __forceinline__ float bf16_bits_to_f32(uint32_t bits16) { return __uint_as_float(bits16 << 16); }
-__device__ __forceinline__ uint32_t f32_to_bf16_bits(float v) {
-    uint32_t u = __float_as_uint(v);
-    if (v != v) return (u >> 16) | 0x0040u;   // NaN stays a (quiet) NaN: the rounding add could carry it into Inf or -0
-    u += 0x7fffu + ((u >> 16) & 1u);          // round to nearest even
-    return u >> 16;
-}
 
 // A 16-byte vector of one row, in fp32 and packed: 8 bf16 or 4 fp32 columns.
 template <bool kBf16>
@@ -53,7 +47,7 @@ struct Columns {
 // together; KMAX == 0: any k.  Bound by HBM (1024 tokens x 7168 in bf16: 45 MB in 10.1 us) and, in small batches, by
 // the two dependent loads; fp32 rows took one column per thread and 15 us at 256 tokens x 2048, now 4.8.  How many
 // threads a workgroup has: row_threads.
-template <bool kBf16, int KMAX>
+template <bool kBf16, int KMAX, bool kWeighted>
 __global__ __launch_bounds__(kMaxThreads) void unpermute_vec_kernel(const uint4* __restrict__ y,
                                                                  const int32_t* __restrict__ pair_row,
                                                                  const float* __restrict__ topk_w, int k, int HV,
@@ -68,7 +62,7 @@ __global__ __launch_bounds__(kMaxThreads) void unpermute_vec_kernel(const uint4*
         for (int j = 0; j < KMAX; ++j) {
             rows[j] = j < k ? pair_row[(size_t)t * k + j] : -1;
             if (rows[j] >= cap) rows[j] = -1;
-            ws[j] = j < k ? topk_w[(size_t)t * k + j] : 0.f;
+            ws[j] = !kWeighted ? 1.f : j < k ? topk_w[(size_t)t * k + j] : 0.f;
         }
         for (int c = threadIdx.x; c < HV; c += blockDim.x) {
             uint4 v[KMAX > 0 ? KMAX : 1];
@@ -87,14 +81,14 @@ __global__ __launch_bounds__(kMaxThreads) void unpermute_vec_kernel(const uint4*
             for (int j = 0; j < k; ++j) {
                 const int r = pair_row[(size_t)t * k + j];
                 if (r < 0 || r >= cap) continue;
-                C::add(acc, topk_w[(size_t)t * k + j], y[(size_t)r * HV + c]);
+                C::add(acc, kWeighted ? topk_w[(size_t)t * k + j] : 1.f, y[(size_t)r * HV + c]);
             }
             out[(size_t)t * HV + c] = C::pack(acc);
         }
     }
 }
 
-template <bool kBf16>
+template <bool kBf16, bool kWeighted>
 __global__ __launch_bounds__(kThreads) void unpermute_scalar_kernel(const void* __restrict__ y,
                                                                     const int32_t* __restrict__ pair_row,
                                                                     const float* __restrict__ topk_w, int k, int H,
@@ -108,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void unpermute_scalar_kernel(const void* 
             if (r < 0 || r >= cap) continue;
             const float v = kBf16 ? bf16_bits_to_f32(((const uint16_t*)y)[(size_t)r * H + c])
                                   : ((const float*)y)[(size_t)r * H + c];
-            acc = fmaf(topk_w[(size_t)t * k + j], v, acc);
+            acc = fmaf(kWeighted ? topk_w[(size_t)t * k + j] : 1.f, v, acc);
         }
         if (kBf16) ((uint16_t*)out)[(size_t)t * H + c] = (uint16_t)f32_to_bf16_bits(acc);
         else ((float*)out)[(size_t)t * H + c] = acc;
@@ -132,13 +126,11 @@ inline int row_threads(int T, int k, int hv) {
     return waves((hv + turns - 1) / turns);
 }
 
-}  // namespace
-}  // namespace metro
-
-extern "C" int moe_unpermute(const void* y_perm, const int32_t* pair_row, const float* topk_w, int T, int k, int H,
-                             int dtype, void* out, void* stream) {
-    using namespace metro;
-    if (!y_perm || !pair_row || !topk_w || !out) return METRO_ERR_INVALID_ARG;
+// kWeighted: topk_w; else every weight is 1.
+template <bool kWeighted>
+int combine(const void* y_perm, const int32_t* pair_row, const float* topk_w, int T, int k, int H, int dtype, void* out, void* stream) {
+    const bool missing = !y_perm || !pair_row || (kWeighted && !topk_w) || !out;
+    if (missing && (kWeighted || T != 0)) return METRO_ERR_INVALID_ARG;
     if (T < 0 || k < 1 || H < 1) return METRO_ERR_INVALID_ARG;
     if (dtype != METRO_DTYPE_BF16 && dtype != METRO_DTYPE_F32) return METRO_ERR_UNSUPPORTED;
     if ((int64_t)T * k >= (1 << 24)) return METRO_ERR_UNSUPPORTED;
@@ -153,19 +145,32 @@ extern "C" int moe_unpermute(const void* y_perm, const int32_t* pair_row, const 
                            (uint4*)out);
     };
     if (H % per == 0 && aligned) {
-        if (bf16 && k <= 8) vec(unpermute_vec_kernel<true, 8>);
-        else if (bf16) vec(unpermute_vec_kernel<true, 0>);
-        else if (k <= 2) vec(unpermute_vec_kernel<false, 2>);          // 8192 tokens x 64, k = 1: 3.8 us, 4.4 with slots for eight
-        else if (k <= 8) vec(unpermute_vec_kernel<false, 8>);
-        else vec(unpermute_vec_kernel<false, 0>);
+        if (bf16 && k <= 8) vec(unpermute_vec_kernel<true, 8, kWeighted>);
+        else if (bf16) vec(unpermute_vec_kernel<true, 0, kWeighted>);
+        else if (k <= 2) vec(unpermute_vec_kernel<false, 2, kWeighted>);   // 8192 tokens x 64, k = 1: 3.8 us, 4.4 with slots for eight
+        else if (k <= 8) vec(unpermute_vec_kernel<false, 8, kWeighted>);
+        else vec(unpermute_vec_kernel<false, 0, kWeighted>);
     } else if (bf16) {
-        hipLaunchKernelGGL(unpermute_scalar_kernel<true>, dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
+        hipLaunchKernelGGL((unpermute_scalar_kernel<true, kWeighted>), dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
                            k, H, out);
     } else {
-        hipLaunchKernelGGL(unpermute_scalar_kernel<false>, dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
+        hipLaunchKernelGGL((unpermute_scalar_kernel<false, kWeighted>), dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
                            k, H, out);
     }
     return hipGetLastError() == hipSuccess ? METRO_OK : METRO_ERR_HIP;
+}
+
+}  // namespace
+}  // namespace metro
+
+extern "C" int moe_unpermute(const void* y_perm, const int32_t* pair_row, const float* topk_w, int T, int k, int H,
+                             int dtype, void* out, void* stream) {
+    return metro::combine<true>(y_perm, pair_row, topk_w, T, k, H, dtype, out, stream);
+}
+
+extern "C" int moe_permute_rows_backward(const void* dx_perm, const int32_t* pair_row, int T, int k, int H, int dtype, void* dx,
+                                         void* stream) {
+    return metro::combine<false>(dx_perm, pair_row, nullptr, T, k, H, dtype, dx, stream);
 }
 
 extern "C" const char* metro_status_string(int status) {
