@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "fp8_common.h"
+#include "fp8_ring.h"
 #include "fp8_split.h"
 #include "metro.h"
 
@@ -29,6 +30,19 @@ __global__ __launch_bounds__(kFp8Threads, 2) void fp8_narrow_kernel(Fp8Args a, i
         if (it.tile.rows <= 16) fp8_tile<kGateUp, kQuantX, OT, 1, 2, kRagged>(a, it.tile, lds);
         else fp8_tile<kGateUp, kQuantX, OT, 2, 1, kRagged>(a, it.tile, lds);
         __syncthreads();                                             // the next item's sums reuse the LDS
+    }
+}
+
+template <bool kGateUp, typename OT>
+__global__ __launch_bounds__(kRingThreads, 2) void fp8_ring_kernel(RingArgs a) {
+    const int xcd = blockIdx.x & 7;
+    RingList list;
+    const int n = list.read(a.group_offsets, a.groups, a.T * a.k, xcd, a.ntn);
+    for (int id = blockIdx.x >> 3; id < n; id += gridDim.x >> 3) {
+        const Tile t = list.tile(id, xcd);
+        if (t.rows <= 32) fp8_ring_tile<kGateUp, OT, 2>(a, t);
+        else if (t.rows <= 64) fp8_ring_tile<kGateUp, OT, 4>(a, t);
+        else fp8_ring_tile<kGateUp, OT, 8>(a, t);
     }
 }
 
@@ -53,6 +67,27 @@ int launch(Fp8Args a, int dtype, hipStream_t st) {
     return launched();
 }
 
+// Ring tiles address rows and a slot's weights in 32 bits.
+bool ring_fits(const Fp8Args& a, bool gate_up) {
+    const uint64_t rows = a.perm_pair ? a.T : (uint64_t)a.T * a.k;
+    return a.K % kBlock == 0 && a.n_out % kBlock == 0 && rows * a.ldx < (1ull << 32) && (uint64_t)a.n_out * (gate_up ? 2 : 1) * a.ldw < (1ull << 32);
+}
+
+constexpr int kRingGrid = 4096;
+template <bool kGateUp, typename OT>
+int launch_ring(RingArgs a, hipStream_t st) {
+    const int cols = kGateUp ? 128 : 256;
+    a.ntn = (a.n_out + cols - 1) / cols;
+    const int cap = a.T * a.k;
+    const int64_t tiles = std::min<int64_t>(cap, max_tiles(cap, a.groups, kRingTileRows));
+    const int64_t per_xcd = a.ntn < 8 ? (tiles * a.ntn + 7) / 8 : tiles * ((a.ntn + 7) / 8);
+    const uint32_t grid = (uint32_t)std::min<int64_t>(8 * per_xcd, kRingGrid);
+    hipLaunchKernelGGL((fp8_ring_kernel<kGateUp, OT>), dim3(grid), dim3(kRingThreads), 0, st, a);
+    return launched();
+}
+
+constexpr int kRingPairs = 2048;            // more rows than this at most: ring tiles
+
 constexpr int kMaxSide = 1 << 20;           // K, columns
 constexpr int kMaxPitch = 1 << 28;          // eight rows are addressed in 32 bits
 
@@ -70,6 +105,8 @@ int check_matrix(const void* p, int ld, int K, const float* scale) {
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// Between the two products: fp32, or (ring tiles) e4m3 and scales, which is less.
 inline size_t act_bytes(int T, int k, int I) { return align256((size_t)T * k * up16(I) * 4); }
 
 }  // namespace
@@ -84,6 +121,11 @@ extern "C" int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const
     if (T == 0) return METRO_OK;
     if (check_matrix(x, ldx, K, xs) != METRO_OK || check_matrix(w, ldw, K, ws) != METRO_OK || !y || misaligned(y)) return METRO_ERR_INVALID_ARG;
     const Fp8Args a{x, xs, perm_pair, group_offsets, (const uint8_t*)w, ws, y, ldx, T, k, groups, K, N, ldw, N, 0};
+    if ((int64_t)T * k > kRingPairs && dtype == METRO_DTYPE_BF16 && ring_fits(a, false)) {
+        RingArgs r{};
+        (Fp8Args&)r = a;
+        return launch_ring<false, __bf16>(r, (hipStream_t)stream);
+    }
     return launch<false, false>(a, dtype, (hipStream_t)stream);
 }
 
@@ -105,6 +147,19 @@ extern "C" int moe_grouped_ffn_fp8(const void* x, int ldx, const float* xs, cons
         return METRO_ERR_INVALID_ARG;
     if (ws_bytes < moe_grouped_ffn_fp8_workspace_bytes(T, k, spr, H, I)) return METRO_ERR_WORKSPACE;
     const int ld_act = (int)up16(I);
+    const int cap = T * k;
+    if (cap > kRingPairs && H % kBlock == 0 && I % kBlock == 0 && dtype == METRO_DTYPE_BF16) {
+        uint8_t* act = (uint8_t*)ws;
+        float* act_scale = (float*)((char*)ws + align256((size_t)cap * I));
+        RingArgs up{}, down{};
+        (Fp8Args&)up = Fp8Args{x, xs, perm_pair, group_offsets, (const uint8_t*)w13, s13, nullptr, ldx, T, k, spr, H, I, ldw13, I, 0};
+        up.act = act, up.act_scale = act_scale;
+        (Fp8Args&)down = Fp8Args{act, act_scale, nullptr, group_offsets, (const uint8_t*)w2, s2, y_perm, I, T, k, spr, I, H, ldw2, H, 0};
+        if (ring_fits(up, true) && ring_fits(down, false)) {
+            rc = launch_ring<true, float>(up, (hipStream_t)stream);
+            return rc != METRO_OK ? rc : launch_ring<false, __bf16>(down, (hipStream_t)stream);
+        }
+    }
     const Fp8Args up{x, xs, perm_pair, group_offsets, (const uint8_t*)w13, s13, ws, ldx, T, k, spr, H, I, ldw13, ld_act, 0};
     rc = launch<true, false>(up, METRO_DTYPE_F32, (hipStream_t)stream);
     if (rc != METRO_OK) return rc;

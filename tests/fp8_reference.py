@@ -54,7 +54,18 @@ def product(x, w):
     return x @ w.T, bound * (np.abs(x) @ np.abs(w).T)
 
 
-def ffn(x, w13, w2):
+def product_many(x, w):
+    """As `product` where the matrix cores multiply e4m3 values themselves (16-bit results of many rows): they align the 128 products of a
+    block to the largest and drop what lies more than 13 binary places below it, so each is off by at most 2^-13 of the largest."""
+    y, err = product(x, w)
+    for k in range(0, x.shape[1], BLOCK):
+        a, b = np.abs(x[:, k:k + BLOCK]), np.abs(w[:, k:k + BLOCK])
+        most = np.stack([(r * b).max(axis=1) for r in a])           # largest product of every pair of rows
+        err = err + BLOCK * 2.0 ** -13 * most
+    return y, err
+
+
+def ffn(x, w13, w2, product=product):
     """One expert on rows x [R,H] (values): (y [R,H], how far it may be off before y itself is rounded).
 
     The activation is requantized.  Its fp32 error moves a value by at most `da`, and the block's maximum likewise, so its e4m3 value

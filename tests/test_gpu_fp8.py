@@ -139,7 +139,7 @@ def offsets_of(sizes):
     return np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
 
 
-def run_mm(sizes, K, N, dtype, rows=None, seed=0):
+def run_mm(sizes, K, N, dtype, rows=None, seed=0, product=ref.product):
     import torch
 
     from paper_2512_09277_amd import api
@@ -157,9 +157,11 @@ def run_mm(sizes, K, N, dtype, rows=None, seed=0):
     assert (got[n:] == -7).all()                                    # rows past the last group stay as they were
     for l, (a, b) in enumerate(zip(off, off[1:])):
         if b > a:
-            want, err = ref.product(xv[a:b], wv[l])
+            want, err = product(xv[a:b], wv[l])
             off_by = np.abs(got[a:b] - want) - ref.rounded(want, err, dtype == "bf16")
             assert (off_by <= 0).all(), (l, off_by.max())
+            # half a step of the result's type, and a hundredth of that for the sums
+            assert np.linalg.norm(got[a:b] - want) <= 1.01 * (ref.UBF16 if dtype == "bf16" else 64 * ref.U32) * np.linalg.norm(want)
     return y
 
 
@@ -175,6 +177,16 @@ def test_product(sizes, K, N, dtype):
 def test_product_of_more_rows_than_a_launch_has_workgroups():
     run_mm([700, 0, 1300, 41], 256, 1024, "bf16")
     run_mm([64, 64] + [30] * 62, 128, 2048, "f32")
+
+
+MANY = 2100                                                         # rows of a batch from which on the tiles are those for many rows
+
+
+@pytest.mark.parametrize("sizes,K,N", [
+    ([1], 128, 128), ([0, 5, 0, 17], 256, 384), ([32, 33, 31], 384, 256), ([64, 65, 63], 512, 640), ([128, 129, 127], 640, 128), ([97, 96], 768, 256),
+    ([300, 0, 1, 513], 896, 384), ([40], 1024, 2176), ([200], 2048, 256), ([1100, 1000], 128, 256), ([20] * 64, 1152, 128)])
+def test_product_of_many_rows(sizes, K, N):
+    run_mm(sizes, K, N, "bf16", rows=max(MANY, sum(sizes)), product=ref.product_many)
 
 
 def test_product_of_token_rows():
@@ -289,6 +301,49 @@ def test_ffn(T, k, H, I, sizes, dtype):
     args, xv, v13, w2v, perm = ffn_case(T, k, H, I, sizes, dtype)
     y = api.moe_grouped_ffn_fp8(**args)
     check_ffn(wide(y), xv, v13, w2v, perm, k, sizes, dtype)
+
+
+@pytest.mark.parametrize("T,k,H,I,sizes", [
+    (1100, 2, 128, 128, [1]), (1100, 2, 256, 384, [3, 0, 32, 33]), (1100, 2, 512, 256, [64, 65, 0, 1]), (1100, 2, 640, 128, [128, 129, 127]),
+    (1100, 2, 896, 640, [300, 20, 513, 60]), (1200, 2, 256, 256, [2300, 0, 100]), (600, 4, 384, 1152, [30] * 20), (2200, 1, 2048, 256, [90, 7])])
+def test_ffn_of_many_rows(T, k, H, I, sizes):
+    """Products of e4m3 values (see ref.product_many).  Element by element, what that bound lets happen to the activation: at worst most
+    values move over an e4m3 border, a step of up to 2^-3 of themselves.  Over the rows of a group the norm tells more: sums of 128
+    products of normal values are off by 1.5e-5 rms (the instruction's, measured), which moves a value over a border with a probability of
+    about 1.5e-5 / 2^-4 by 2^-4 of itself, sqrt(2.4e-4) * 2^-4 = 1e-3 of the norm, beside 2^-8 at most for the rounding to bf16.  A single
+    row can be off by more: one of its largest activations moved is 2^-3 of that one."""
+    from paper_2512_09277_amd import api
+
+    print(f"ffn of many rows T={T} k={k} H={H} I={I} sizes={sizes}", flush=True)
+    args, xv, v13, w2v, perm = ffn_case(T, k, H, I, sizes, "bf16")
+    got = wide(api.moe_grouped_ffn_fp8(**args))
+    off = offsets_of(sizes)
+    assert (got[off[-1]:] == -7).all()
+    for l, (a, b) in enumerate(zip(off, off[1:])):
+        if b > a:
+            want, err = ref.ffn(xv[perm[a:b] // k], v13[l], w2v[l], product=ref.product_many)
+            off_by = np.abs(got[a:b] - want) - ref.rounded(want, err, True)
+            assert (off_by <= 0).all(), (l, off_by.max())
+            if b - a >= 30:
+                assert np.linalg.norm(got[a:b] - want) <= (ref.UBF16 + 1e-3) * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("T,k,H,I,sizes,dtype", [
+    (1100, 2, 256, 128, [40, 0, 150, 3], "f32"), (2200, 1, 200, 128, [17, 33], "bf16"), (1100, 2, 128, 72, [20, 5], "bf16")])
+def test_ffn_of_many_rows_in_other_forms(T, k, H, I, sizes, dtype):
+    """fp32 results and odd sizes keep the tiles for few rows, whose activation between the products is fp32; so does a full batch."""
+    from paper_2512_09277_amd import api
+
+    args, xv, v13, w2v, perm = ffn_case(T, k, H, I, sizes, dtype)
+    check_ffn(wide(api.moe_grouped_ffn_fp8(**args)), xv, v13, w2v, perm, k, sizes, dtype)
+    sizes = [T * k]
+    args, xv, v13, w2v, perm = ffn_case(T, k, H, I, sizes, dtype)
+    import torch
+
+    need = api.moe_grouped_ffn_fp8_workspace_bytes(T, k, 1, H, I)
+    guard = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
+    check_ffn(wide(api.moe_grouped_ffn_fp8(**args, ws=guard[:need])), xv, v13, w2v, perm, k, sizes, dtype)
+    assert (guard[need:] == 0x5a).all()
 
 
 def test_ffn_without_rows():
