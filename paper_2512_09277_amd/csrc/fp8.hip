@@ -33,17 +33,17 @@ __global__ __launch_bounds__(kFp8Threads, 2) void fp8_narrow_kernel(Fp8Args a, i
     }
 }
 
+// A workgroup per CU; each takes every n-th item of its XCD's list, big ones first.
+constexpr int kRingGrid = 256;
 template <bool kGateUp, typename OT>
 __global__ __launch_bounds__(kRingThreads, 2) void fp8_ring_kernel(RingArgs a) {
-    const int xcd = blockIdx.x & 7;
     RingList list;
-    const int n = list.read(a.group_offsets, a.groups, a.T * a.k, xcd, a.ntn);
-    for (int id = blockIdx.x >> 3; id < n; id += gridDim.x >> 3) {
-        const Tile t = list.tile(id, xcd);
-        if (t.rows <= 32) fp8_ring_tile<kGateUp, OT, 2>(a, t);
-        else if (t.rows <= 64) fp8_ring_tile<kGateUp, OT, 4>(a, t);
-        else fp8_ring_tile<kGateUp, OT, 8>(a, t);
-    }
+    int n[2];
+    list.read(a.group_offsets, a.groups, a.T * a.k, blockIdx.x & 7, a.ntn, n);
+    const int step = gridDim.x >> 3, id = blockIdx.x >> 3;
+    fp8_ring_items<kGateUp, OT, 0>(a, list, id, n[0], step);
+    __syncthreads();                                                 // the other class has other places in LDS
+    fp8_ring_items<kGateUp, OT, 1>(a, list, (id + step - n[0] % step) % step, n[1], step);       // in turn behind them
 }
 
 inline int launched() { return hipGetLastError() == hipSuccess ? METRO_OK : METRO_ERR_HIP; }
@@ -73,7 +73,6 @@ bool ring_fits(const Fp8Args& a, bool gate_up) {
     return a.K % kBlock == 0 && a.n_out % kBlock == 0 && rows * a.ldx < (1ull << 32) && (uint64_t)a.n_out * (gate_up ? 2 : 1) * a.ldw < (1ull << 32);
 }
 
-constexpr int kRingGrid = 4096;
 template <bool kGateUp, typename OT>
 int launch_ring(RingArgs a, hipStream_t st) {
     const int cols = kGateUp ? 128 : 256;

@@ -10,6 +10,10 @@
 // One barrier per step.  When step s begins its fragments are in registers; behind the barrier -- every wave has read all of stage s,
 // and stage s + 1 has arrived -- the stage is refilled with step s + D, the fragments of s + 1 are read, and s is multiplied.
 // The wait before the barrier is a count of newer loads, so these are unconditional: past the end every lane takes the same bytes.
+//
+// A workgroup has a CU for itself, so nothing else runs while a tile begins or ends: the last D steps of a tile therefore load the first
+// D of the workgroup's next one.  Step j of it goes where step j of any tile is expected, stage j % D, which is free in that of the
+// last steps that has the same remainder.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -24,7 +28,6 @@ namespace {
 
 constexpr int kRingThreads = 512;
 constexpr int kRingTileRows = 128;
-constexpr int kBand = 8;                    // tiles of a slot that are taken through all columns of an XCD together
 
 // LDS: 18 units of 8 KB, two of 4 KB, the scales of four stages.
 template <int I>
@@ -40,6 +43,12 @@ __device__ __forceinline__ float* ring_scale() {            // of 128 rows, then
     return scale;
 }
 
+template <int I>
+__device__ __forceinline__ uint32_t* ring_part() {          // a row's maximum in each of four waves
+    __shared__ __attribute__((aligned(16))) uint32_t part[kRingTileRows * 4];
+    return part;
+}
+
 template <int n>
 __device__ __forceinline__ void wait_all_but() {        // outstanding vector loads at most n, no LDS access outstanding
     static_assert(n < 64, "");
@@ -53,60 +62,91 @@ struct RingArgs : Fp8Args {
 
 // Unit of 64 rows (at most) of a stage's activations.
 template <int MT>
-constexpr int x_unit(int stage, int p) { return MT == 2 ? 16 + stage : 12 + stage * (MT / 4) + p; }
+constexpr int x_unit(int stage, int p) { return MT == 2 ? 16 + stage : 12 + stage * 2 + p; }
 
-template <bool kGateUp, typename OT, int MT>
-__device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t) {
-    constexpr int M2 = MT / 2, D = MT == 2 ? 4 : 3, kXUnits = MT == 8 ? 2 : 1;
+// Where the loads of a tile come from.
+template <bool kGateUp, int kXUnits>
+struct RingSource {
+    const uint8_t* w;           // the slot's weights
+    const float* scale;         // rows' scales (two waves) or the weights'
+    uint32_t w_lane, w_at[4];   // of unit p, this lane's row of the tile's weights
+    uint32_t x_lane[kXUnits], s_lane;
+
+    static __device__ __forceinline__ int row_of(int p) {           // of the tile, whose 16 bytes this lane loads to unit p
+        return p * 64 + (kXUnits == 1 ? (threadIdx.x >> 3) & 31 : threadIdx.x >> 3);
+    }
+    // Rows are loaded a tile ahead of their use (`raw`), for they may hang on a load of their own.
+    struct Raw { int row[kXUnits], scale_row; };
+    static __device__ __forceinline__ Raw raw(const RingArgs& a, const Tile& t) {
+        auto source = [&](int r) {                                  // past the tile: its last row
+            const int row = t.row0 + min(r, t.rows - 1);
+            return a.perm_pair ? a.perm_pair[row] : row;
+        };
+        Raw r;
+#pragma unroll
+        for (int p = 0; p < kXUnits; ++p) r.row[p] = source(row_of(p));
+        r.scale_row = source((int)(threadIdx.x & 127));
+        return r;
+    }
+    __device__ __forceinline__ void set(const RingArgs& a, const Tile& t, const Raw& raw, int wv) {
+        const int nb = a.K / kBlock, col0 = t.col * (kGateUp ? 128 : 256), piece = ((threadIdx.x & 7) ^ ((threadIdx.x >> 3) & 7)) * 16;
+        auto token = [&](int r) { return (uint32_t)(a.perm_pair ? min(max(r / a.k, 0), a.T - 1) : r); };
+        const int second = kGateUp ? blocks_of(a.n_out) : col0 + 128 < a.n_out ? 1 : 0;
+        w = a.w + (size_t)t.slot * (size_t)(kGateUp ? 2 * (int64_t)a.n_out : a.n_out) * a.ldw;
+        // Row i of wave tx's 16 rows in unit p is column 64 tx + 16 (i / 4) + 4 p + i % 4 of the tile; gate/up: units 0, 1 gate, 2, 3 up,
+        // column 32 tx + 8 (i / 4) + 4 (p % 2) + i % 4 of either.  A lane then ends up with 16 (8) neighbouring columns of a row, and the
+        // lanes of a wave with whole lines.  Past the last column: the tile's first half again.
+        const int i = (threadIdx.x >> 3) & 15, tx = threadIdx.x >> 7, in = kGateUp ? tx : second ? tx : tx & 1;
+        w_lane = (uint32_t)(kGateUp ? in * 32 + (i >> 2) * 8 + (i & 3) : in * 64 + (i >> 2) * 16 + (i & 3)) * (uint32_t)a.ldw + piece;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) w_at[p] = (uint32_t)(kGateUp ? (p >> 1) * a.n_out + col0 + (p & 1) * 4 : col0 + p * 4) * (uint32_t)a.ldw;
+#pragma unroll
+        for (int p = 0; p < kXUnits; ++p) x_lane[p] = token(raw.row[p]) * (uint32_t)a.ldx + piece;
+        // Two waves load the scales of 64 rows each, the others those of the weights: gate's and up's, or of columns 0..127 and
+        // 128..255 (if there are any).  Six waves load the same, which costs less than a branch in the loop.
+        const int row_blocks = blocks_of(a.n_out) * (kGateUp ? 2 : 1);
+        scale = wv < 2 ? a.xs : a.ws + ((size_t)t.slot * row_blocks + col0 / kBlock) * nb;
+        s_lane = (wv < 2 ? token(raw.scale_row) : (uint32_t)((threadIdx.x & 1) * second)) * (uint32_t)(nb * 4);
+    }
+};
+
+// ready: the first D stages are in LDS or on their way.  has_next: the last steps load those of `then`.
+template <bool kGateUp, typename OT, int MT, typename Source>
+__device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, const Source& now, const Source& then, bool ready, bool has_next) {
+    constexpr bool kBig = MT > 2;
+    constexpr int M2 = MT / 2, D = kBig ? 3 : 4, kXUnits = kBig ? 2 : 1;
     constexpr int kUnitLoads = 4 + kXUnits, kLoads = kUnitLoads + 1;    // of a stage, per lane
     static_assert(MT == 2 || MT == 4 || MT == 8, "");
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, q = lane >> 4, tx = wv & 3, ty = wv >> 2;
     const int nb = a.K / kBlock, col0 = t.col * (kGateUp ? 128 : 256);
-    const int piece = ((tid & 7) ^ ((tid >> 3) & 7)) * 16;
-
-    // unit p of a stage: weight rows w_row(p) ..+ 63; gate/up: two of gate, two of up.  Past the last column: the tile's first again
-    auto w_row = [&](int p) { return kGateUp ? (p >> 1) * a.n_out + col0 + (p & 1) * 64 : col0 + p * 64 < a.n_out ? col0 + p * 64 : col0; };
-    const uint8_t* wslot = a.w + (size_t)t.slot * (size_t)(kGateUp ? 2 * (int64_t)a.n_out : a.n_out) * a.ldw;
-    const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)wslot, 0, -1, 0x00027000);
-    const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)a.x, 0, -1, 0x00027000);
-    uint32_t w_at[4];
-#pragma unroll
-    for (int p = 0; p < 4; ++p) w_at[p] = (uint32_t)w_row(p) * (uint32_t)a.ldw;
-    const uint32_t w_lane = (uint32_t)(tid >> 3) * (uint32_t)a.ldw + piece;
-    auto source = [&](int r) {                              // past the tile: its last row
-        const int row = t.row0 + min(r, t.rows - 1);
-        return (uint32_t)(a.perm_pair ? min(max(a.perm_pair[row] / a.k, 0), a.T - 1) : row);
-    };
-    uint32_t x_lane[kXUnits];
-#pragma unroll
-    for (int p = 0; p < kXUnits; ++p) x_lane[p] = source(p * 64 + (MT == 2 ? (tid >> 3) & 31 : tid >> 3)) * (uint32_t)a.ldx + piece;
-    // Scales: two waves load those of 64 rows each, the others those of the weights: gate's and up's, or of columns 0..127 and
-    // 128..255 (if there are any).  Six waves load the same, which costs less than a branch in the loop.
-    const int row_blocks = blocks_of(a.n_out) * (kGateUp ? 2 : 1), second = kGateUp ? blocks_of(a.n_out) : col0 + 128 < a.n_out ? 1 : 0;
-    const size_t ws_slot = (size_t)t.slot * row_blocks + col0 / kBlock;
-    const __amdgpu_buffer_rsrc_t s_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(wv < 2 ? a.xs : a.ws + ws_slot * nb), 0, -1, 0x00027000);
-    const uint32_t s_lane = (wv < 2 ? source(wv * 64 + lane) : (uint32_t)((lane & 1) * second)) * (uint32_t)(nb * 4);
     const int s_at = min(wv, 2) * 64;
 
-    // piece p of a stage's loads: scales first, then the units
-    auto load = [&](auto U, auto P, int s) {
+    // A load of step s: of this tile, of the next one's step `first` (s % D), or of nothing new.
+    struct From { __amdgpu_buffer_rsrc_t w, scale; int at; bool own, real; };
+    const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)a.x, 0, -1, 0x00027000);
+    auto from = [&](int s, int first) {
+        const bool own = s < nb;
+        return From{__builtin_amdgcn_make_buffer_rsrc((void*)(own ? now.w : then.w), 0, -1, 0x00027000),
+                    __builtin_amdgcn_make_buffer_rsrc((void*)(own ? now.scale : then.scale), 0, -1, 0x00027000), own ? s : min(first, nb - 1), own,
+                    own || has_next};
+    };
+    auto load = [&](auto U, auto P, const From& f) {
         constexpr int set = decltype(U)::value % D, p = decltype(P)::value;
-        const bool real = s < nb;
-        const int step = min(s, nb - 1);
         if constexpr (p < 4) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (__attribute__((address_space(3))) void*)(ring_unit<set * 4 + p>() + wv * 1024), 16,
-                                                     (int)(real ? w_lane : 0u), (int)(w_at[p] + step * kBlock), 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(f.w, (__attribute__((address_space(3))) void*)(ring_unit<set * 4 + p>() + wv * 1024), 16,
+                                                     (int)(!f.real ? 0u : f.own ? now.w_lane : then.w_lane), (int)((f.own ? now.w_at[p] : then.w_at[p]) + f.at * kBlock), 0, 0);
         } else {
+            const uint32_t lane_at = f.own ? now.x_lane[p - 4] : then.x_lane[p - 4];
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                x_rsrc, (__attribute__((address_space(3))) void*)(ring_unit<x_unit<MT>(set, p - 4)>() + (MT == 2 ? wv & 3 : wv) * 1024), 16,
-                (int)(real ? x_lane[p - 4] : 0u), step * kBlock, 0, 0);
+                x_rsrc, (__attribute__((address_space(3))) void*)(ring_unit<x_unit<MT>(set, p - 4)>() + (kBig ? wv : wv & 3) * 1024), 16,
+                (int)(f.real ? lane_at : 0u), f.at * kBlock, 0, 0);
         }
     };
-    auto load_scale = [&](auto U, int s) {
+    auto load_scale = [&](auto U, const From& f) {
         constexpr int set = decltype(U)::value % D;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(s_rsrc, (__attribute__((address_space(3))) void*)(ring_scale<set>() + s_at), 4, (int)s_lane,
-                                                 min(s, nb - 1) * 4, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(f.scale, (__attribute__((address_space(3))) void*)(ring_scale<set>() + s_at), 4,
+                                                 (int)(f.own ? now.s_lane : then.s_lane), f.at * 4, 0, 0);
     };
     const int rd = r16 * 128 + ((q ^ (r16 & 7)) * 16);
     i32x8 fw[4], fx[M2];                                    // each is replaced once it has been multiplied
@@ -126,11 +166,22 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t) {
         fx[mt] = fragment(ring_unit<x_unit<MT>(set, mt >> 1)>() + ((mt & 1) * 2 + ty) * 2048);
     };
     floatx4 acc[4][M2];
-    auto multiply = [&](auto B, auto M, float scale) {
-        constexpr int b = decltype(B)::value, mt = decltype(M)::value;
-        const floatx4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[b], fx[mt], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+    // A product is added two products later: its result takes longer than the next one to be issued.
+    constexpr int kProducts = 4 * M2, kLate = 2;
+    floatx4 late[kLate] = {};
+    float late_scale[kLate] = {};
+    auto add_late = [&](auto I) {                                   // product I (of this step, or counted back into the last one)
+        constexpr int i = (decltype(I)::value + kProducts) % kProducts, slot = (decltype(I)::value + kProducts) % kLate;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) acc[b][mt][v] = fmaf(p[v], scale, acc[b][mt][v]);
+        for (int v = 0; v < 4; ++v) acc[i / M2][i % M2][v] = fmaf(late[slot][v], late_scale[slot], acc[i / M2][i % M2][v]);
+    };
+    auto multiply = [&](auto I, float scale) {
+        constexpr int i = decltype(I)::value, slot = i % kLate;
+        const floatx4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i / M2], fx[i % M2], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+        add_late(std::integral_constant<int, i - kLate>{});
+        late[slot] = p;
+        late_scale[slot] = scale;
+        __builtin_amdgcn_sched_barrier(0);
     };
     auto arrive = [&](auto Left) {
         __builtin_amdgcn_sched_barrier(0);
@@ -139,50 +190,62 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t) {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    float xscale[M2], wscale[2];
+    float xscale[M2], wscale[kGateUp ? 2 : 1];
     auto read_scale = [&](auto U) {
         constexpr int set = decltype(U)::value % D;
 #pragma unroll
         for (int mt = 0; mt < M2; ++mt) xscale[mt] = ring_scale<set>()[mt * 32 + ty * 16 + r16];
-        wscale[0] = ring_scale<set>()[128];
-        wscale[1] = ring_scale<set>()[129];
+        wscale[0] = ring_scale<set>()[kGateUp ? 128 : 128 + (tx >> 1)];
+        if constexpr (kGateUp) wscale[1] = ring_scale<set>()[129];
     };
     // The loads of step s + D go out between the products: a burst of them in front would hold the products back.
     auto step = [&](auto U, int s) {
         constexpr int u = decltype(U)::value;
         constexpr std::integral_constant<int, u + 1> next{};
-        float scale[2][M2];
+        float scale[kGateUp ? 2 : 1][M2];
 #pragma unroll
-        for (int mt = 0; mt < M2; ++mt) scale[0][mt] = xscale[mt] * wscale[0], scale[1][mt] = xscale[mt] * wscale[1];
+        for (int mt = 0; mt < M2; ++mt) {
+            scale[0][mt] = xscale[mt] * wscale[0];
+            if constexpr (kGateUp) scale[1][mt] = xscale[mt] * wscale[1];
+        }
+        const From f = from(s + D, u % D);
         arrive(std::integral_constant<int, (D - 2) * kLoads>{});
         read_scale(next);
-        load_scale(U, s + D);
+        load_scale(U, f);
         run_steps(std::make_integer_sequence<int, 4>{}, [&](auto B, int) {
             constexpr int b = decltype(B)::value;
             run_steps(std::make_integer_sequence<int, M2>{}, [&](auto M, int) {
                 constexpr int mt = decltype(M)::value, at = b * M2 + mt;
-                multiply(B, M, scale[b >> 1][mt]);
+                multiply(std::integral_constant<int, at>{}, scale[kGateUp ? b >> 1 : 0][mt]);
                 if constexpr (b == 3) read_x(next, M);
-                constexpr int from = at * kUnitLoads / (4 * M2), to = (at + 1) * kUnitLoads / (4 * M2);
-                if constexpr (to > from) load(U, std::integral_constant<int, from>{}, s + D);
-                if constexpr (to > from + 1) load(U, std::integral_constant<int, from + 1>{}, s + D);
+                constexpr int begin = at * kUnitLoads / (4 * M2), end = (at + 1) * kUnitLoads / (4 * M2);
+                if constexpr (end > begin) load(U, std::integral_constant<int, begin>{}, f);
+                if constexpr (end > begin + 1) load(U, std::integral_constant<int, begin + 1>{}, f);
             }, 0);
             read_w(next, B);
             __builtin_amdgcn_sched_barrier(0);
         }, 0);
     };
     asm volatile("; ring of %0 stages, %1 loads each" ::"i"(D), "i"(kLoads));      // a comment in the assembly, no instruction
-    run_steps(std::make_integer_sequence<int, D>{}, [&](auto U, int s) {
-        load_scale(U, s);
-        run_steps(std::make_integer_sequence<int, kUnitLoads>{}, [&](auto P, int) { load(U, P, s); }, 0);
-        __builtin_amdgcn_sched_barrier(0);                  // the waits count on this order
-    }, 0);
+    if (!ready) {
+        run_steps(std::make_integer_sequence<int, D>{}, [&](auto U, int s) {
+            const From f{__builtin_amdgcn_make_buffer_rsrc((void*)now.w, 0, -1, 0x00027000),
+                         __builtin_amdgcn_make_buffer_rsrc((void*)now.scale, 0, -1, 0x00027000), min(s, nb - 1), true, true};
+            load_scale(U, f);
+            run_steps(std::make_integer_sequence<int, kUnitLoads>{}, [&](auto P, int) { load(U, P, f); }, 0);
+            __builtin_amdgcn_sched_barrier(0);              // the waits count on this order
+        }, 0);
+        wait_all_but<(D - 1) * kLoads>();
+    }
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int mt = 0; mt < M2; ++mt) acc[b][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
     constexpr std::integral_constant<int, 0> first{};
-    arrive(std::integral_constant<int, (D - 1) * kLoads>{});
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
     read_scale(first);
     run_steps(std::make_integer_sequence<int, M2>{}, [&](auto M, int) { read_x(first, M); }, 0);
     run_steps(std::make_integer_sequence<int, 4>{}, [&](auto B, int) { read_w(first, B); }, 0);
@@ -190,14 +253,18 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t) {
     int s = 0;
     for (; s + kPeriod <= nb; s += kPeriod) run_steps(std::make_integer_sequence<int, kPeriod>{}, step, s);
     run_steps_tail(std::make_integer_sequence<int, kPeriod - 1>{}, step, s, nb);
-    wait_all_but<0>();                                      // nothing is on its way to LDS when the workgroup ends or goes on
-    asm volatile("; ring done");
+    add_late(std::integral_constant<int, -2>{});
+    add_late(std::integral_constant<int, -1>{});
+    // The next tile's stages have arrived before anything else is issued, so that it need not wait for this one's results to be
+    // stored; without one, nothing is on its way to LDS when the workgroup ends.
+    __builtin_amdgcn_sched_barrier(0);
+    wait_all_but<0>();
+    asm volatile("; ring done" ::: "memory");
 
     if constexpr (kGateUp) {
         // Columns col0 .. col0 + 127 are one block of the activation: its maximum over the lanes of a row, then over four waves.
         float o[2][M2][4];
-        __syncthreads();
-        uint32_t* part = reinterpret_cast<uint32_t*>(ring_unit<0>());       // [row][wave]
+        uint32_t* const part = ring_part<0>();
 #pragma unroll
         for (int mt = 0; mt < M2; ++mt) {
             uint32_t m = 0;
@@ -221,36 +288,39 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t) {
             const BlockScale sc = block_scale(max(max(m[0], m[1]), max(m[2], m[3])));
             if (row >= t.rows) continue;
             const size_t out = (size_t)(t.row0 + row);
+            u32x2 v;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
-                *reinterpret_cast<uint32_t*>(a.act + out * a.ldd + col0 + b * 64 + tx * 16 + q * 4) =
-                    pack_e4m3(o[b][mt][0] * sc.inverse, o[b][mt][1] * sc.inverse, o[b][mt][2] * sc.inverse, o[b][mt][3] * sc.inverse);
+                v[b] = pack_e4m3(o[b][mt][0] * sc.inverse, o[b][mt][1] * sc.inverse, o[b][mt][2] * sc.inverse, o[b][mt][3] * sc.inverse);
+            *reinterpret_cast<u32x2*>(a.act + out * a.ldd + col0 + tx * 32 + q * 8) = v;
             if (tx == 0 && q == 0) a.act_scale[out * (a.n_out / kBlock) + t.col] = sc.scale;
         }
-        __syncthreads();                                    // the next tile's loads take the LDS
     } else {
 #pragma unroll
         for (int mt = 0; mt < M2; ++mt) {
             const int row = mt * 32 + ty * 16 + r16;
             if (row >= t.rows) continue;
+            const int col = col0 + tx * 64 + q * 16;
+            if (col >= a.n_out) continue;
+            OT* out = reinterpret_cast<OT*>(a.dst) + (size_t)(t.row0 + row) * a.ldd + col;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int col = col0 + b * 64 + tx * 16 + q * 4;
-                const float o[4] = {acc[b][mt][0], acc[b][mt][1], acc[b][mt][2], acc[b][mt][3]};
-                if (col < a.n_out) store_columns(reinterpret_cast<OT*>(a.dst) + (size_t)(t.row0 + row) * a.ldd + col, 4, true, o);
-            }
+            for (int b = 0; b < 4; b += 2)
+                *reinterpret_cast<u32x4*>(out + b * 4) = u32x4{pack_bf16x2(acc[b][mt][0], acc[b][mt][1]), pack_bf16x2(acc[b][mt][2], acc[b][mt][3]),
+                                                               pack_bf16x2(acc[b + 1][mt][0], acc[b + 1][mt][1]), pack_bf16x2(acc[b + 1][mt][2], acc[b + 1][mt][3])};
         }
-        __syncthreads();
     }
 }
 
-// All tiles of 128 rows (the last of a slot shorter) x column tiles.  Workgroup i runs on XCD i mod 8, each with an L2 of its own: the
-// tiles of a column of one slot read the same weights, so they are neighbours in the list of one XCD, and the columns of a slot go
-// round the XCDs.  With fewer columns than XCDs the items themselves go round.  Lane = slot.
+// A slot's rows make tiles of 128 rows and one for the remainder: big ones (more than 32 rows) and at most one small one.  Workgroup i runs
+// on XCD i mod 8, each with an L2 of its own: the tiles of a column of one slot read the same weights, so they are neighbours in the
+// list of one XCD, and the columns of a slot go round the XCDs.  With fewer columns than XCDs the items themselves go round.
+// Lane = slot.
+constexpr int kSmallRows = 32;
 struct RingList {
-    int begin, rows, tiles, first, mine, incl, stride;
+    int begin, rows, first, stride, xcd;
+    int tiles[2], incl[2];                      // of big ones, small ones: tiles of the slot, items of the slots up to it
 
-    __device__ __forceinline__ int read(const int32_t* __restrict__ group_offsets, int groups, int cap, int xcd, int n_cols) {
+    __device__ __forceinline__ void read(const int32_t* __restrict__ group_offsets, int groups, int cap, int xcd_, int n_cols, int (&n)[2]) {
         const int l = lane_id();
         int m = 0;
         begin = 0;
@@ -259,30 +329,60 @@ struct RingList {
             m = min(max(group_offsets[l + 1], begin), cap) - begin;
         }
         rows = m;
-        tiles = (m + kRingTileRows - 1) / kRingTileRows;
+        xcd = xcd_;
+        const int part = m & (kRingTileRows - 1);
+        tiles[0] = m / kRingTileRows + (part > kSmallRows);
+        tiles[1] = part > 0 && part <= kSmallRows;
         stride = n_cols < 8 ? 1 : 8;
         first = n_cols < 8 ? 0 : (xcd - l * n_cols) & 7;
-        mine = tiles * (n_cols < 8 ? n_cols : (n_cols - first + 7) >> 3);
-        incl = wave_inclusive_sum(mine);
-        const int n = __builtin_amdgcn_readlane(incl, kWave - 1);
-        return n_cols < 8 ? (n - xcd + 7) >> 3 : n;
+        const int cols = n_cols < 8 ? n_cols : (n_cols - first + 7) >> 3;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            incl[c] = wave_inclusive_sum(tiles[c] * cols);
+            n[c] = __builtin_amdgcn_readlane(incl[c], kWave - 1);
+            if (n_cols < 8) n[c] = (n[c] - xcd + 7) >> 3;
+        }
     }
-    __device__ __forceinline__ Tile tile(int nth, int xcd) const {
-        const int i = stride == 1 ? nth * 8 + xcd : nth;
-        const uint64_t owner = __ballot(incl - mine <= i && i < incl);             // exactly one lane
+    template <int kClass>
+    __device__ __forceinline__ Tile tile(int nth) const {
+        const int i = stride == 1 ? nth * 8 + xcd : nth, before = __shfl_up(incl[kClass], 1), from = lane_id() ? before : 0;
+        const uint64_t owner = __ballot(from <= i && i < incl[kClass]);            // exactly one lane
         const int o = __ffsll((unsigned long long)owner) - 1;
-        const int n = __builtin_amdgcn_readlane(tiles, o), at = i - __builtin_amdgcn_readlane(incl - mine, o);
-        const int cols = (uint32_t)__builtin_amdgcn_readlane(mine, o) / (uint32_t)n;
-        const int band = (uint32_t)at / (uint32_t)(kBand * cols), height = min(kBand, n - band * kBand), in = at - band * kBand * cols;
-        const int c = (uint32_t)in / (uint32_t)height, row = (band * kBand + in - c * height) * kRingTileRows;
+        const int n = __builtin_amdgcn_readlane(tiles[kClass], o), at = i - __builtin_amdgcn_readlane(from, o), m = __builtin_amdgcn_readlane(rows, o);
+        const int c = (uint32_t)at / (uint32_t)n, row = kClass ? m / kRingTileRows * kRingTileRows : (at - c * n) * kRingTileRows;
         Tile t;
         t.slot = o;
         t.col = __builtin_amdgcn_readlane(first, o) + c * stride;
         t.row0 = __builtin_amdgcn_readlane(begin, o) + row;
-        t.rows = min(kRingTileRows, __builtin_amdgcn_readlane(rows, o) - row);
+        t.rows = min(kRingTileRows, m - row);
         return t;
     }
 };
+
+// The items id, id + step, ... of a class.
+template <bool kGateUp, typename OT, int kClass>
+__device__ __forceinline__ void fp8_ring_items(const RingArgs& a, const RingList& list, int id, int n, int step) {
+    using Source = RingSource<kGateUp, kClass ? 1 : 2>;
+    if (id >= n) return;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Tile t = list.tile<kClass>(id), t1 = id + step < n ? list.tile<kClass>(id + step) : t;
+    Source now, then;
+    now.set(a, t, Source::raw(a, t), wv);
+    typename Source::Raw raw = Source::raw(a, t1);
+    for (bool ready = false;; ready = true) {
+        const bool more = id + step < n;
+        then.set(a, t1, raw, wv);
+        const Tile t2 = id + 2 * step < n ? list.tile<kClass>(id + 2 * step) : t1;
+        raw = Source::raw(a, t2);
+        if constexpr (kClass == 1) fp8_ring_tile<kGateUp, OT, 2>(a, t, now, then, ready, more);
+        else if (t.rows <= 64) fp8_ring_tile<kGateUp, OT, 4>(a, t, now, then, ready, more);
+        else fp8_ring_tile<kGateUp, OT, 8>(a, t, now, then, ready, more);
+        if (!more) return;
+        id += step;
+        t = t1, t1 = t2;
+        now = then;
+    }
+}
 
 }  // namespace
 }  // namespace metro

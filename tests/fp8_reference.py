@@ -59,8 +59,8 @@ def product_many(x, w):
     block to the largest and drop what lies more than 13 binary places below it, so each is off by at most 2^-13 of the largest."""
     y, err = product(x, w)
     for k in range(0, x.shape[1], BLOCK):
-        a, b = np.abs(x[:, k:k + BLOCK]), np.abs(w[:, k:k + BLOCK])
-        most = np.stack([(r * b).max(axis=1) for r in a])           # largest product of every pair of rows
+        # the largest product of a pair of rows is at most that of their largest values
+        most = np.abs(x[:, k:k + BLOCK]).max(axis=1)[:, None] * np.abs(w[:, k:k + BLOCK]).max(axis=1)[None]
         err = err + BLOCK * 2.0 ** -13 * most
     return y, err
 

@@ -8,4 +8,4 @@ def test_needed_stages_have_arrived(tmp_path):
         weak, rings = weak_waits(lines)
         assert not weak, (name, weak)
         found |= rings
-    assert found == {(4, 6), (3, 6), (3, 7)}                        # up to 32, 64 and 128 rows
+    assert found == {(4, 6), (3, 7)}                                # small and big tiles

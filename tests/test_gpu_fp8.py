@@ -189,6 +189,15 @@ def test_product_of_many_rows(sizes, K, N):
     run_mm(sizes, K, N, "bf16", rows=max(MANY, sum(sizes)), product=ref.product_many)
 
 
+@pytest.mark.parametrize("K", [128, 256, 384, 512, 640, 1152])
+def test_product_of_more_tiles_than_workgroups(K):
+    """A workgroup's next tile is loaded by the last steps of the one before: steps fewer than the stages of the ring, as many, more; big
+    tiles of both kinds and small ones, a change from the ones to the others, fewer columns than XCDs and more."""
+    run_mm([7000, 1500, 70, 1, 20, 45, 8, 300], K, 1024, "bf16", product=ref.product_many)
+    run_mm([2900, 40, 1, 129, 31], K, 2304, "bf16", product=ref.product_many)
+    run_mm([20, 3, 31, 0] * 16, K, 2176, "bf16", rows=2400, product=ref.product_many)
+
+
 def test_product_of_token_rows():
     """perm_pair names the token of a row; entries out of range are clamped, offsets that are no partition too."""
     import torch
@@ -305,7 +314,7 @@ def test_ffn(T, k, H, I, sizes, dtype):
 
 @pytest.mark.parametrize("T,k,H,I,sizes", [
     (1100, 2, 128, 128, [1]), (1100, 2, 256, 384, [3, 0, 32, 33]), (1100, 2, 512, 256, [64, 65, 0, 1]), (1100, 2, 640, 128, [128, 129, 127]),
-    (1100, 2, 896, 640, [300, 20, 513, 60]), (1200, 2, 256, 256, [2300, 0, 100]), (600, 4, 384, 1152, [30] * 20), (2200, 1, 2048, 256, [90, 7])])
+    (1100, 2, 896, 640, [300, 20, 513, 60]), (1500, 4, 256, 1152, [2000, 1000, 40, 7, 33, 900, 20]), (1200, 2, 256, 256, [2300, 0, 100]), (600, 4, 384, 1152, [30] * 20), (2200, 1, 2048, 256, [90, 7])])
 def test_ffn_of_many_rows(T, k, H, I, sizes):
     """Products of e4m3 values (see ref.product_many).  Element by element, what that bound lets happen to the activation: at worst most
     values move over an e4m3 border, a step of up to 2^-3 of themselves.  Over the rows of a group the norm tells more: sums of 128
