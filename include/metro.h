@@ -271,9 +271,10 @@ int moe_quantize_weights_fp8(const void* w, int ldw, int slots, int rows, int K,
 /*
  * moe_grouped_mm_fp8 -- rows sorted by group (expert) times the weights of their group.  For row r of group l, with blocks b of K:
  *     y[r][n] = sum over b of xs[r][b] * ws[l][n/128][b] * (sum over k in b of x[r][k] * w[l][n][k])
- * products and sums in fp32, in a fixed order.  METRO_DTYPE_BF16 results of batches of more than 2048 rows (T*k), where K and N are
- * multiples of 128, sum the products of a block in the matrix cores' e4m3 form, which drops what lies more than 13 binary places below
- * the block's largest product (1.5e-5 of the sum for normal values); blocks are added in fp32.  Only groups with at least one row are
+ * products and sums in fp32, in a fixed order.  METRO_DTYPE_BF16 results of many rows (T*k > 4096 with perm_pair; without it T*k >
+ * 32*groups and T*k*N >= 2^21), where K and N are multiples of 128, sum the products of a block in the matrix cores' e4m3 form, which
+ * drops what lies more than 13 binary places below the block's largest product (1.5e-5 of the sum for normal values); blocks are added
+ * in fp32.  Only groups with at least one row are
  * touched.  The gradient of x is the same call with transposed weights and scales on quantized rows of dy.
  *
  *   x      e4m3, xs float32     perm_pair NULL: [T*k,K], row r itself;  else [T,K], row r is that of token perm_pair[r] / k
@@ -287,7 +288,7 @@ int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const int32_t* p
 
 /*
  * moe_grouped_ffn_fp8 -- moe_grouped_ffn on 8-bit experts.  For row r of local slot l, token t = perm_pair[r] / k:
- *     gate, up = x[t] . w13[l]^T          (as in moe_grouped_mm_fp8)
+ *     gate, up = x[t] . w13[l]^T          (as in moe_grouped_mm_fp8 with perm_pair)
  *     act = silu(gate) * up in fp32, then to e4m3 with a scale for each 128 as by moe_quantize_fp8
  *     y_perm[r] = act . w2[l]^T
  *

@@ -16,8 +16,8 @@
 namespace metro {
 namespace {
 
-constexpr int kNarrowRows32 = 32;
-constexpr int kNarrowGrid = 1536;           // three rounds of the 512 resident workgroups, the rest in turns
+constexpr int kNarrowRows32 = 32;           // of a K-split tile
+constexpr int kNarrowGrid = 2560;           // five rounds of the 512 resident workgroups, the rest in turns
 
 template <bool kGateUp, bool kQuantX, typename OT, bool kRagged>
 __global__ __launch_bounds__(kFp8Threads, 2) void fp8_narrow_kernel(Fp8Args a, int64_t n_items) {
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(kFp8Threads, 2) void fp8_narrow_kernel(Fp8Args a, i
     for (int64_t id = blockIdx.x; id < n_items; id += gridDim.x) {
         const Item it = locate_in_order(a.group_offsets, a.groups, a.T * a.k, kNarrowRows32, a.ntn, id);
         if (!it.valid) return;                                       // uniform; items are consecutive
-        if (it.tile.rows <= 16) fp8_tile<kGateUp, kQuantX, OT, 1, 2, kRagged>(a, it.tile, lds);
+        if (it.tile.rows <= 16) fp8_tile<kGateUp, kQuantX, OT, 1, 1, kRagged>(a, it.tile, lds);
         else fp8_tile<kGateUp, kQuantX, OT, 2, 1, kRagged>(a, it.tile, lds);
         __syncthreads();                                             // the next item's sums reuse the LDS
     }
@@ -85,7 +85,18 @@ int launch_ring(RingArgs a, hipStream_t st) {
     return launched();
 }
 
-constexpr int kRingPairs = 2048;            // more rows than this at most: ring tiles
+// Ring tiles for batches of many rows.  With token lists the host knows T * k, of which a rank of eight has an eighth: more than 4096.
+// Measured, the FFN of such a rank, K-split / ring tiles, us: 512 tokens (k = 8) 35 / 36 at 2048 x 768, 103 / 100 at 4096 x 1536, 299 / 310 at
+// 7168 x 2048; 256 tokens 29 / 34, 84 / 88, 272 / 293; 768 and 640 tokens 43 / 39, 104 / 93, 321 / 318 (1024 of the last: 466 / 326).
+constexpr int kRingPairs = 4096;
+// Rows in order are all there.  More than one K-split tile a group, and at least 1024 items of these, two for every workgroup that can
+// be resident.  Measured, K-split / ring tiles, us: one group of 4096 x 4096, 256 rows 18 / 27, 512 rows 32 / 28; of 2048 x 7168, 512 and 1024
+// rows 28 / 44 and 50 / 44; of 512 x 1024, 2048 rows 7.8 / 11.9; 16 groups of 2048 x 1024, 512 and 1024 rows 9.1 / 10.3 and 13.5 / 11.8; 32
+// groups of 4096 x 4096, 1024 and 2048 rows 107 / 128 and 157 / 135.
+bool many_rows(const Fp8Args& a) {
+    const int64_t cap = (int64_t)a.T * a.k;
+    return a.perm_pair ? cap > kRingPairs : cap > kNarrowRows32 * a.groups && cap * a.n_out >= (1 << 21);
+}
 
 constexpr int kMaxSide = 1 << 20;           // K, columns
 constexpr int kMaxPitch = 1 << 28;          // eight rows are addressed in 32 bits
@@ -120,7 +131,7 @@ extern "C" int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const
     if (T == 0) return METRO_OK;
     if (check_matrix(x, ldx, K, xs) != METRO_OK || check_matrix(w, ldw, K, ws) != METRO_OK || !y || misaligned(y)) return METRO_ERR_INVALID_ARG;
     const Fp8Args a{x, xs, perm_pair, group_offsets, (const uint8_t*)w, ws, y, ldx, T, k, groups, K, N, ldw, N, 0};
-    if ((int64_t)T * k > kRingPairs && dtype == METRO_DTYPE_BF16 && ring_fits(a, false)) {
+    if (many_rows(a) && dtype == METRO_DTYPE_BF16 && ring_fits(a, false)) {
         RingArgs r{};
         (Fp8Args&)r = a;
         return launch_ring<false, __bf16>(r, (hipStream_t)stream);

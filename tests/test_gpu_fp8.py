@@ -179,14 +179,16 @@ def test_product_of_more_rows_than_a_launch_has_workgroups():
     run_mm([64, 64] + [30] * 62, 128, 2048, "f32")
 
 
-MANY = 2100                                                         # rows of a batch from which on the tiles are those for many rows
+def many(sizes, N):
+    """Rows of a batch that takes the tiles for many rows."""
+    return max(sum(sizes), 32 * len(sizes) + 1, -(-(1 << 21) // N))
 
 
 @pytest.mark.parametrize("sizes,K,N", [
     ([1], 128, 128), ([0, 5, 0, 17], 256, 384), ([32, 33, 31], 384, 256), ([64, 65, 63], 512, 640), ([128, 129, 127], 640, 128), ([97, 96], 768, 256),
     ([300, 0, 1, 513], 896, 384), ([40], 1024, 2176), ([200], 2048, 256), ([1100, 1000], 128, 256), ([20] * 64, 1152, 128)])
 def test_product_of_many_rows(sizes, K, N):
-    run_mm(sizes, K, N, "bf16", rows=max(MANY, sum(sizes)), product=ref.product_many)
+    run_mm(sizes, K, N, "bf16", rows=many(sizes, N), product=ref.product_many)
 
 
 @pytest.mark.parametrize("K", [128, 256, 384, 512, 640, 1152])
@@ -195,7 +197,7 @@ def test_product_of_more_tiles_than_workgroups(K):
     tiles of both kinds and small ones, a change from the ones to the others, fewer columns than XCDs and more."""
     run_mm([7000, 1500, 70, 1, 20, 45, 8, 300], K, 1024, "bf16", product=ref.product_many)
     run_mm([2900, 40, 1, 129, 31], K, 2304, "bf16", product=ref.product_many)
-    run_mm([20, 3, 31, 0] * 16, K, 2176, "bf16", rows=2400, product=ref.product_many)
+    run_mm([20, 3, 31, 0] * 16, K, 2176, "bf16", rows=many([20, 3, 31, 0] * 16, 2176), product=ref.product_many)
 
 
 def test_product_of_token_rows():
@@ -313,8 +315,9 @@ def test_ffn(T, k, H, I, sizes, dtype):
 
 
 @pytest.mark.parametrize("T,k,H,I,sizes", [
-    (1100, 2, 128, 128, [1]), (1100, 2, 256, 384, [3, 0, 32, 33]), (1100, 2, 512, 256, [64, 65, 0, 1]), (1100, 2, 640, 128, [128, 129, 127]),
-    (1100, 2, 896, 640, [300, 20, 513, 60]), (1500, 4, 256, 1152, [2000, 1000, 40, 7, 33, 900, 20]), (1200, 2, 256, 256, [2300, 0, 100]), (600, 4, 384, 1152, [30] * 20), (2200, 1, 2048, 256, [90, 7])])
+    (2100, 2, 128, 128, [1]), (2100, 2, 256, 384, [3, 0, 32, 33]), (2100, 2, 512, 256, [64, 65, 0, 1]), (2100, 2, 640, 128, [128, 129, 127]),
+    (2100, 2, 896, 640, [300, 20, 513, 60]), (1500, 4, 256, 1152, [2000, 1000, 40, 7, 33, 900, 20]), (2200, 2, 256, 256, [4300, 0, 100]),
+    (1100, 4, 384, 1152, [30] * 20), (4200, 1, 2048, 256, [90, 7])])
 def test_ffn_of_many_rows(T, k, H, I, sizes):
     """Products of e4m3 values (see ref.product_many).  Element by element, what that bound lets happen to the activation: at worst most
     values move over an e4m3 border, a step of up to 2^-3 of themselves.  Over the rows of a group the norm tells more: sums of 128
@@ -338,7 +341,7 @@ def test_ffn_of_many_rows(T, k, H, I, sizes):
 
 
 @pytest.mark.parametrize("T,k,H,I,sizes,dtype", [
-    (1100, 2, 256, 128, [40, 0, 150, 3], "f32"), (2200, 1, 200, 128, [17, 33], "bf16"), (1100, 2, 128, 72, [20, 5], "bf16")])
+    (2100, 2, 256, 128, [40, 0, 150, 3], "f32"), (4200, 1, 200, 128, [17, 33], "bf16"), (2100, 2, 128, 72, [20, 5], "bf16")])
 def test_ffn_of_many_rows_in_other_forms(T, k, H, I, sizes, dtype):
     """fp32 results and odd sizes keep the tiles for few rows, whose activation between the products is fp32; so does a full batch."""
     from paper_2512_09277_amd import api
