@@ -1,6 +1,7 @@
 // moe_quantize_fp8 and moe_quantize_weights_fp8: rows to e4m3 with a scale for each 128 values of a row, weights to e4m3 with a scale for
 // each 128 x 128.  One pass: a block stays in registers between its maximum and its rounding, so every byte is read and written once,
-// and HBM bounds both.
+// and HBM bounds both: 16384 rows of 7168 in bf16, 352 MB, 63 us, 5.6 TB/s (67 us with at most 4096 workgroups); weights of 18 x 1536 x
+// 2048 in bf16, 170 MB, 34.6 us, 4.9 TB/s (39.5 with the values widened to fp32 in registers), 1.06 GB of them 197 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -9,7 +10,6 @@
 
 #include "fp8_common.h"
 #include "metro.h"
-#include "row_vec.h"
 
 namespace metro {
 namespace {
@@ -17,25 +17,41 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPer = 8;                     // values of a lane: 16 lanes are a block of a row
 
-// kPer values from column `c` of a row; kVec: 16-byte loads, all inside the row; else element by element, zeros past the end.
+// Memory at any element alignment; the hardware takes unaligned 128-bit global loads.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// kPer values from column `c` of a row, as they are in memory.  kVec: rows are whole, aligned groups of kPer; else any rows, with zeros
+// past the end.  A lane of quantize_weights_kernel holds 64 values from its maximum to its rounding: in 16 bits half the registers.
 template <bool kBf16, bool kVec>
-__device__ __forceinline__ void load_values(const void* row, int c, int K, float (&f)[kPer]) {
-    if constexpr (kVec && kBf16) {
-        RowVec<true, 8>::widen(reinterpret_cast<const uint4*>(row)[c / 8], f);
-    } else if constexpr (kVec) {
-        float a[4], b[4];
-        RowVec<false, 4>::widen(reinterpret_cast<const uint4*>(row)[c / 4], a);
-        RowVec<false, 4>::widen(reinterpret_cast<const uint4*>(row)[c / 4 + 1], b);
+struct Values {
+    static constexpr int kLoads = kBf16 ? 1 : 2;
+    u32x4 raw[kLoads];
+
+    __device__ __forceinline__ void load(const void* row, int c, int K) {
+        const char* p = reinterpret_cast<const char*>(row) + (size_t)c * (kBf16 ? 2 : 4);
+        if (kVec || c + kPer <= K) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = a[e], f[4 + e] = b[e];
-    } else {
+            for (int i = 0; i < kLoads; ++i) {
+                if constexpr (kVec) raw[i] = reinterpret_cast<const u32x4*>(p)[i];
+                else raw[i] = reinterpret_cast<const u32x4_any*>(p)[i];
+            }
+        } else {                                            // the last values of a row
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            f[e] = 0.f;
-            if (c + e < K) f[e] = kBf16 ? bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(row)[c + e]) : reinterpret_cast<const float*>(row)[c + e];
+            for (int e = 0; e < kPer; ++e) {
+                if (c + e >= K) continue;
+                if constexpr (kBf16) raw[0][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
+                else raw[e >> 2][e & 3] = reinterpret_cast<const uint32_t*>(p)[e];
+            }
         }
     }
-}
+    __device__ __forceinline__ void widen(float (&f)[kPer]) const {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            if constexpr (kBf16) f[e] = __uint_as_float(e & 1 ? raw[0][e >> 1] & 0xffff0000u : raw[0][e >> 1] << 16);
+            else f[e] = __uint_as_float(raw[e >> 2][e & 3]);
+        }
+    }
+};
 
 // q rows are 16-byte aligned, so a lane's eight bytes are too.
 __device__ __forceinline__ void store_values(uint8_t* row, int c, int K, const float (&f)[kPer], float inverse) {
@@ -67,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const void* __r
     const int64_t n = (int64_t)rows * nb, stride = (int64_t)gridDim.x * (kTurns * kThreads / 16);
     const int c16 = (threadIdx.x & 15) * kPer;
     for (int64_t first = (int64_t)blockIdx.x * (kTurns * kThreads / 16) + threadIdx.x / 16; first < n; first += stride) {
-        float f[kTurns][kPer];
+        Values<kBf16, kVec> f[kTurns];
         int row[kTurns], col[kTurns];
 #pragma unroll
         for (int u = 0; u < kTurns; ++u) {
@@ -75,18 +91,16 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const void* __r
             row[u] = (int)(n >> 32 ? i / nb : (int64_t)((uint32_t)i / (uint32_t)nb));
             col[u] = (int)(i - (int64_t)row[u] * nb);
             const int c = col[u] * kBlock + c16;
-            if (kVec && c >= K) {                                               // a short last block
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) f[u][e] = 0.f;
-            } else {
-                load_values<kBf16, kVec>(reinterpret_cast<const char*>(x) + row[u] * row_bytes, c, K, f[u]);
-            }
+            f[u] = {};
+            if (c < K) f[u].load(reinterpret_cast<const char*>(x) + row[u] * row_bytes, c, K);      // else: a short last block
         }
 #pragma unroll
         for (int u = 0; u < kTurns; ++u) {
-            const BlockScale s = block_scale(group_max<16>(largest_of(f[u])));
+            float v[kPer];
+            f[u].widen(v);
+            const BlockScale s = block_scale(group_max<16>(largest_of(v)));
             if (first + u * (kThreads / 16) >= n) continue;
-            store_values(q + (size_t)row[u] * ldq, col[u] * kBlock + c16, K, f[u], s.inverse);
+            store_values(q + (size_t)row[u] * ldq, col[u] * kBlock + c16, K, v, s.inverse);
             if ((threadIdx.x & 15) == 0) scale[(size_t)row[u] * nb + col[u]] = s.scale;
         }
     }
@@ -104,20 +118,20 @@ __global__ __launch_bounds__(kThreads) void quantize_weights_kernel(const void* 
     const int cb = (int)(id - at * nb), slot = (int)(at / nr), rb = (int)(at - (int64_t)slot * nr);
     const int r0 = rb * kBlock + threadIdx.x / 16, c = cb * kBlock + (threadIdx.x & 15) * kPer;
     const int64_t base = (int64_t)slot * rows;
-    float f[kTurns][kPer];
+    Values<kBf16, kVec> f[kTurns];
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
         const int r = r0 + u * 16;
-        if (r >= rows || c >= K) {
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) f[u][e] = 0.f;
-        } else {
-            load_values<kBf16, kVec>(reinterpret_cast<const char*>(w) + (base + r) * row_bytes, c, K, f[u]);
-        }
+        f[u] = {};
+        if (r < rows && c < K) f[u].load(reinterpret_cast<const char*>(w) + (base + r) * row_bytes, c, K);
     }
     uint32_t m = 0;
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u) m = max(m, largest_of(f[u]));
+    for (int u = 0; u < kTurns; ++u) {
+        float v[kPer];
+        f[u].widen(v);
+        m = max(m, largest_of(v));
+    }
     m = group_max<16>(m);
     m = max(m, (uint32_t)__shfl_xor((int)m, 16));
     m = max(m, (uint32_t)__shfl_xor((int)m, 32));
@@ -131,7 +145,10 @@ __global__ __launch_bounds__(kThreads) void quantize_weights_kernel(const void* 
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
         const int r = r0 + u * 16;
-        if (r < rows) store_values(q + (base + r) * (int64_t)ldq, c, K, f[u], s.inverse);
+        if (r >= rows) continue;
+        float v[kPer];
+        f[u].widen(v);
+        store_values(q + (base + r) * (int64_t)ldq, c, K, v, s.inverse);
     }
 }
 
@@ -161,7 +178,7 @@ extern "C" int moe_quantize_fp8(const void* x, int ldx, int R, int K, int dtype,
     const int64_t n = (int64_t)R * blocks_of(K);
     auto go = [&](auto kernel, int turns) {
         const int64_t per = turns * (kThreads / 16);
-        const uint32_t grid = (uint32_t)std::min<int64_t>((n + per - 1) / per, 4096);
+        const uint32_t grid = (uint32_t)std::min<int64_t>((n + per - 1) / per, 1 << 20);
         hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, (hipStream_t)stream, x, (int64_t)ldx * (bf16 ? 2 : 4), R, K, n_rows,
                            (uint8_t*)q, ldq, scale);
     };

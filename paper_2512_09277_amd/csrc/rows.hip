@@ -1,6 +1,8 @@
 // moe_permute_rows and moe_unpermute_backward: tokens sorted by expert, and the gradient of the weighted sum that brings them back.
 // Both walk the tokens, not the sorted rows: a token's row is then read once for all its pairs here, and the dot products of the
-// weights' gradient stay inside one workgroup.  Bound by HBM: every byte is read or written once.
+// weights' gradient stay inside one workgroup.  Bound by HBM: every byte is read or written once.  Gradient of the combine, 8192 tokens x
+// 2048 in bf16, k = 8, all pairs here: 571 MB in 117 us, 4.9 TB/s, what a large copy reaches.  Sort of 4096 tokens x 7168 in bf16, batches
+// of 70, 71 and 171 MB: 20 us on average, 5.2 TB/s (22 us with one vector of a lane on its way at a time).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -14,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPairs = 8;                   // pairs of a token that are in registers at a time
+constexpr int kAhead = 4;                   // vectors of a row that a lane loads before it stores the first
 
 // Sum over the lanes of a wave, in every lane; fixed order.
 __device__ __forceinline__ float wave_sum(float v) {
@@ -42,11 +45,18 @@ __global__ __launch_bounds__(kThreads) void permute_rows_kernel(const void* __re
             any |= row[j] >= 0;
         }
         if (!any) continue;
-        for (int c = lane; c < n_vec; c += kLanes) {
-            const auto v = V::load(x, (size_t)t * n_vec + c);
+        for (int c0 = lane; c0 < n_vec; c0 += kLanes * kAhead) {
+            typename V::Raw v[kAhead];
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j)
-                if (row[j] >= 0) V::store(x_perm, (size_t)row[j] * n_vec + c, v);
+            for (int u = 0; u < kAhead; ++u)
+                if (c0 + u * kLanes < n_vec) v[u] = V::load(x, (size_t)t * n_vec + c0 + u * kLanes);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                if (row[j] < 0) continue;                 // uniform per token
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (c0 + u * kLanes < n_vec) V::store(x_perm, (size_t)row[j] * n_vec + c0 + u * kLanes, v[u]);
+            }
         }
     }
 }
@@ -125,13 +135,14 @@ __global__ __launch_bounds__(kThreads) void unpermute_backward_kernel(const void
 }
 
 // f(kBf16, kN, kWaveToken, vectors of a row, workgroups): 16-byte vectors where rows are whole ones, else element by element; a
-// wave per token up to 4 vectors a lane.
+// wave per token up to 2 vectors a lane.  Measured for the gradient of the combine, us, a wave / a workgroup per token: 256 vectors,
+// 8192 and 512 tokens (bf16, k = 8, all pairs here) 133 / 117 and 16.8 / 11.4.
 template <typename F>
 int by_shape(int T, int H, int dtype, bool aligned, F&& f) {
     const int per = dtype == METRO_DTYPE_BF16 ? 8 : 4;
     const bool vec = aligned && H % per == 0;
     const int n_vec = vec ? H / per : H;
-    const bool wave = n_vec <= 256;
+    const bool wave = n_vec <= 128;
     const int grid = wave ? (T + kThreads / 64 - 1) / (kThreads / 64) : T;
     auto pick = [&](auto Bf16, auto N) {
         if (wave) f(Bf16, N, std::true_type{}, n_vec, grid);
