@@ -1,6 +1,6 @@
 // moe_unpermute: one rank's share of the combine step -- a gather of the rows a token owns in
 // y_perm, weighted by the gating weights and summed in fp32 in ascending j.  With all weights 1 it is the gradient of
-// moe_permute_rows (moe_permute_rows_backward).
+// moe_permute_rows over rows of whole vectors.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kMaxThreads) void unpermute_vec_kernel(const uint4*
     }
 }
 
-template <bool kBf16, bool kWeighted>
+template <bool kBf16>
 __global__ __launch_bounds__(kThreads) void unpermute_scalar_kernel(const void* __restrict__ y,
                                                                     const int32_t* __restrict__ pair_row,
                                                                     const float* __restrict__ topk_w, int k, int H,
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void unpermute_scalar_kernel(const void* 
             if (r < 0 || r >= cap) continue;
             const float v = kBf16 ? bf16_bits_to_f32(((const uint16_t*)y)[(size_t)r * H + c])
                                   : ((const float*)y)[(size_t)r * H + c];
-            acc = fmaf(kWeighted ? topk_w[(size_t)t * k + j] : 1.f, v, acc);
+            acc = fmaf(topk_w[(size_t)t * k + j], v, acc);
         }
         if (kBf16) ((uint16_t*)out)[(size_t)t * H + c] = (uint16_t)f32_to_bf16_bits(acc);
         else ((float*)out)[(size_t)t * H + c] = acc;
@@ -126,11 +126,10 @@ inline int row_threads(int T, int k, int hv) {
     return waves((hv + turns - 1) / turns);
 }
 
-// kWeighted: topk_w; else every weight is 1.
+// kWeighted: topk_w; else every weight is 1, rows are whole, aligned vectors.
 template <bool kWeighted>
 int combine(const void* y_perm, const int32_t* pair_row, const float* topk_w, int T, int k, int H, int dtype, void* out, void* stream) {
-    const bool missing = !y_perm || !pair_row || (kWeighted && !topk_w) || !out;
-    if (missing && (kWeighted || T != 0)) return METRO_ERR_INVALID_ARG;
+    if (!y_perm || !pair_row || (kWeighted && !topk_w) || !out) return METRO_ERR_INVALID_ARG;
     if (T < 0 || k < 1 || H < 1) return METRO_ERR_INVALID_ARG;
     if (dtype != METRO_DTYPE_BF16 && dtype != METRO_DTYPE_F32) return METRO_ERR_UNSUPPORTED;
     if ((int64_t)T * k >= (1 << 24)) return METRO_ERR_UNSUPPORTED;
@@ -150,27 +149,29 @@ int combine(const void* y_perm, const int32_t* pair_row, const float* topk_w, in
         else if (k <= 2) vec(unpermute_vec_kernel<false, 2, kWeighted>);   // 8192 tokens x 64, k = 1: 3.8 us, 4.4 with slots for eight
         else if (k <= 8) vec(unpermute_vec_kernel<false, 8, kWeighted>);
         else vec(unpermute_vec_kernel<false, 0, kWeighted>);
+    } else if (!kWeighted) {
+        return METRO_ERR_INVALID_ARG;             // such rows are summed in rows.hip
     } else if (bf16) {
-        hipLaunchKernelGGL((unpermute_scalar_kernel<true, kWeighted>), dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
+        hipLaunchKernelGGL(unpermute_scalar_kernel<true>, dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
                            k, H, out);
     } else {
-        hipLaunchKernelGGL((unpermute_scalar_kernel<false, kWeighted>), dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
+        hipLaunchKernelGGL(unpermute_scalar_kernel<false>, dim3(T), dim3(kThreads), 0, st, y_perm, pair_row, topk_w,
                            k, H, out);
     }
     return hipGetLastError() == hipSuccess ? METRO_OK : METRO_ERR_HIP;
 }
 
 }  // namespace
+
+int sum_whole_rows(const void* dx_perm, const int32_t* pair_row, int T, int k, int H, int dtype, void* dx, void* stream) {
+    return combine<false>(dx_perm, pair_row, nullptr, T, k, H, dtype, dx, stream);
+}
+
 }  // namespace metro
 
 extern "C" int moe_unpermute(const void* y_perm, const int32_t* pair_row, const float* topk_w, int T, int k, int H,
                              int dtype, void* out, void* stream) {
     return metro::combine<true>(y_perm, pair_row, topk_w, T, k, H, dtype, out, stream);
-}
-
-extern "C" int moe_permute_rows_backward(const void* dx_perm, const int32_t* pair_row, int T, int k, int H, int dtype, void* dx,
-                                         void* stream) {
-    return metro::combine<false>(dx_perm, pair_row, nullptr, T, k, H, dtype, dx, stream);
 }
 
 extern "C" const char* metro_status_string(int status) {
