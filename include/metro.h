@@ -254,7 +254,7 @@ int moe_unpermute_backward(const void* dout, const void* y_perm, const int32_t* 
  *   x      [R,K]  dtype    rows ldx >= K elements apart
  *   n_rows [1]    int32    rows to convert, read on the device (clamped to [0, R]); NULL = R.  Rows past it are left as they were
  *   q      [R,K]  e4m3     out, rows ldq bytes apart (bytes past K are not written)
- *   scale  [R, ceil(K/128)] float32 out
+ *   scale  [R, ceil(K/128)] float32 out        Limit: K <= 2^30
  */
 int moe_quantize_fp8(const void* x, int ldx, int R, int K, int dtype, const int32_t* n_rows, void* q, int ldq, float* scale,
                      void* stream);
@@ -264,7 +264,7 @@ int moe_quantize_fp8(const void* x, int ldx, int R, int K, int dtype, const int3
  * pass the gate and up halves as matrices of their own: slots = 2*spr, rows = I.
  *
  *   w [slots,rows,K] dtype, rows ldw elements and slots rows*ldw elements apart; q [slots,rows,K] e4m3 out, likewise with ldq bytes;
- *   scale [slots, ceil(rows/128), ceil(K/128)] float32 out.       Limit: fewer than 2^24 blocks.
+ *   scale [slots, ceil(rows/128), ceil(K/128)] float32 out.       Limits: rows, K <= 2^30, fewer than 2^24 blocks.
  */
 int moe_quantize_weights_fp8(const void* w, int ldw, int slots, int rows, int K, int dtype, void* q, int ldq, float* scale, void* stream);
 

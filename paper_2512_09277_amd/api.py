@@ -495,7 +495,7 @@ def _fp8_matrix(t: torch.Tensor, name: str):
     k16 = (K + 15) // 16 * 16
     one = rows <= 1
     ld = t.stride(-2) if not one else t.stride(0) if t.dim() == 3 and lead > 1 else k16
-    if (K > 1 and t.stride(-1) != 1) or ld < K or ld % 16 or (t.dim() == 3 and lead > 1 and t.stride(0) != rows * ld):
+    if (K > 1 and t.stride(-1) != 1) or ld < K or ld % 16 or ld >= 1 << 31 or (t.dim() == 3 and lead > 1 and t.stride(0) != rows * ld):
         raise TypeError(f"{name}: rows must be K-contiguous, a multiple of 16 bytes apart (strides {t.stride()})")
     if t.numel() and t.storage_offset() + (lead * rows - 1) * ld + k16 > t.untyped_storage().nbytes():
         raise ValueError(f"{name}: the last row must be readable up to a multiple of 16 bytes")
@@ -530,7 +530,7 @@ def moe_quantize_fp8(x: torch.Tensor, n_rows: Optional[torch.Tensor] = None,
     if out is None:
         out = quantize_buffers(R, K, x.device)
     _on_current_device(x=x, n_rows=n_rows, q=out["q"], scale=out["scale"])
-    if not x.is_cuda or (K > 1 and x.stride(1) != 1) or (R > 1 and x.stride(0) < K):
+    if not x.is_cuda or (K > 1 and x.stride(1) != 1) or (R > 1 and not K <= x.stride(0) < 1 << 31):
         raise TypeError(f"x: expected a device tensor with contiguous rows, got strides {x.stride()} on {x.device}")
     q, ldq = _fp8_matrix(_shaped(out["q"], (R, K), "q"), "q")
     nr = None if n_rows is None else _dev(_shaped(n_rows, (1,), "n_rows"), torch.int32, "n_rows")
@@ -548,6 +548,8 @@ def moe_quantize_weights_fp8(w: torch.Tensor, out: Optional[Dict[str, torch.Tens
         out = quantize_weights_buffers(S, rows, K, w.device)
     _on_current_device(w=w, q=out["q"], scale=out["scale"])
     p, ld = _weights(w, w.dtype, "w")
+    if ld >= 1 << 31:
+        raise TypeError(f"w: rows are too far apart (strides {w.stride()})")
     q, ldq = _fp8_matrix(_shaped(out["q"], (S, rows, K), "q"), "q")
     _check(load().moe_quantize_weights_fp8(p, ld, S, rows, K, code, q, ldq,
                                            _dev(_shaped(out["scale"], (S, _blocks(rows), _blocks(K)), "scale"), torch.float32, "scale"),

@@ -157,7 +157,10 @@ bool whole_vectors(const void* p, int64_t ld, int K, int dtype) {
     return ((uintptr_t)p & 15) == 0 && ld % per == 0 && K % 8 == 0;
 }
 
+constexpr int kMaxSide = 1 << 30;           // rows, K: block counts stay inside 32 bits
+
 int check_types(int ld, int K, int dtype, const void* q, int ldq) {
+    if (K > kMaxSide) return METRO_ERR_UNSUPPORTED;
     if (K < 1 || ld < K || ldq < K || ldq % 16 != 0 || ((uintptr_t)q & 15) != 0) return METRO_ERR_INVALID_ARG;
     if (dtype != METRO_DTYPE_BF16 && dtype != METRO_DTYPE_F32) return METRO_ERR_UNSUPPORTED;
     return METRO_OK;
@@ -197,8 +200,8 @@ extern "C" int moe_quantize_weights_fp8(const void* w, int ldw, int slots, int r
     if (rc != METRO_OK) return rc;
     if (slots == 0) return METRO_OK;
     if (!w || !q || !scale) return METRO_ERR_INVALID_ARG;
-    const int64_t n = (int64_t)slots * blocks_of(rows) * blocks_of(K);
-    if (n >= (1 << 24)) return METRO_ERR_UNSUPPORTED;                           // a launch has fewer than 2^32 threads
+    const int64_t n = rows > kMaxSide ? 0 : (int64_t)slots * blocks_of(rows) * blocks_of(K);
+    if (rows > kMaxSide || n >= (1 << 24)) return METRO_ERR_UNSUPPORTED;                           // a launch has fewer than 2^32 threads
     const bool bf16 = dtype == METRO_DTYPE_BF16, vec = whole_vectors(w, ldw, K, dtype);
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((uint32_t)n), dim3(kThreads), 0, (hipStream_t)stream, w, (int64_t)ldw * (bf16 ? 2 : 4), rows, K,

@@ -226,6 +226,62 @@ def test_product_of_token_rows():
     assert torch.equal(z[same], y[same])
 
 
+@pytest.mark.parametrize("offsets", [[-4, 900, 100000], [700, 300, 20000], [0, 16000, 16384], [16384, 16384, 16384]])
+def test_offsets_that_are_no_partition(offsets):
+    """Batches of many rows: what offsets past the batch name is left out, and nothing outside y is written."""
+    import torch
+
+    from paper_2512_09277_amd import api
+
+    rng = np.random.default_rng(9)
+    K, N, rows = 256, 128, 16384
+    x, xs, _ = quantized(rng, (rows, K))
+    w, ws, _ = quantized(rng, (2, N, K), 128)
+    clean = [max(0, min(o, rows)) for o in offsets]
+    for l in (1, 2):
+        clean[l] = max(clean[l - 1], clean[l]) if offsets[l] >= offsets[l - 1] else clean[l]
+    guard = torch.full((rows + 256, N), -7.0, dtype=torch.bfloat16, device="cuda")
+    api.moe_grouped_mm_fp8(x, xs, dev(np.array(offsets, np.int32)), w, ws, y=guard[128:128 + rows])
+    assert (guard[:128] == -7).all() and (guard[128 + rows:] == -7).all() and torch.isfinite(guard.float()).all()
+    if sorted(offsets) == offsets:
+        want = torch.full((rows, N), -7.0, dtype=torch.bfloat16, device="cuda")
+        api.moe_grouped_mm_fp8(x, xs, dev(np.array(clean, np.int32)), w, ws, y=want)
+        assert torch.equal(guard[128:128 + rows], want)
+
+
+def test_offsets_past_32_bits():
+    """Rows of x and weights of a group that start more than 4 GiB behind their first."""
+    import torch
+
+    from paper_2512_09277_amd import api
+
+    rng = np.random.default_rng(10)
+    K, N, T = 8192, 128, (1 << 19) + 40
+    far, fs, fv = quantized(rng, (40, K))
+    w, ws, wv = quantized(rng, (1, N, K), 128, 0.02)
+    x = torch.zeros((T, K), dtype=torch.uint8, device="cuda").view(api.FP8)
+    x[T - 40:].copy_(far)
+    xs = torch.zeros((T, K // 128), device="cuda")
+    xs[T - 40:] = fs
+    perm = torch.full((T,), T - 1, dtype=torch.int32, device="cuda")
+    perm[:40] = torch.arange(T - 40, T, dtype=torch.int32)
+    off = dev(np.array([0, 40], np.int32))
+    y = api.moe_grouped_mm_fp8(x, xs, off, w, ws, dtype=torch.float32, perm_pair=perm)
+    want, err = ref.product(fv, wv[0])
+    assert (np.abs(wide(y[:40]) - want) <= ref.rounded(want, err, False)).all()
+    del x, xs, perm, y
+    G, M = 65 - 1, 8200
+    big = torch.zeros((G, M, K), dtype=torch.uint8, device="cuda").view(api.FP8)       # 4.3 GB; the last group's last rows count
+    big[G - 1, M - N:].copy_(w[0])
+    scale = torch.zeros((G, (M + 127) // 128, K // 128), device="cuda")
+    scale[G - 1, (M - N) // 128:] = 1
+    off = torch.zeros(G + 1, dtype=torch.int32, device="cuda")
+    off[G] = 40
+    y = api.moe_grouped_mm_fp8(far, fs, off, big, scale, dtype=torch.float32)
+    want, err = ref.product(fv, wide(w[0]))
+    assert (np.abs(wide(y[:, M - N:]) - want) <= ref.rounded(want, err, False)).all() and not y[:, :M - N].any()
+
+
 def test_values_that_are_not_finite_stay_in_their_rows_and_columns():
     import torch
 

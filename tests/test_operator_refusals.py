@@ -34,11 +34,12 @@ def test_sorted_rows(lib):  # noqa: F811
 
 def test_quantize(lib):  # noqa: F811
     refusals(lib.moe_quantize_fp8, [P, 200, 4, 200, 1, NONE, P, 208, P, NONE],
-             [(0, NONE, -1), (1, 199, -1), (2, -1, -1), (3, 0, -1), (4, 3, -2), (6, NONE, -1), (6, ODD, -1), (7, 192, -1), (7, 201, -1), (8, NONE, -1)])
+             [(0, NONE, -1), (1, 199, -1), (2, -1, -1), (3, 0, -1), (4, 3, -2), (6, NONE, -1), (6, ODD, -1), (7, 192, -1), (7, 201, -1), (8, NONE, -1),
+              (3, (1 << 30) + 1, -2)])
     assert lib.moe_quantize_fp8(P, 200, 0, 200, 1, NONE, P, 208, P, NONE) == 0
     refusals(lib.moe_quantize_weights_fp8, [P, 200, 2, 50, 200, 0, P, 208, P, NONE],
              [(0, NONE, -1), (1, 199, -1), (2, -1, -1), (3, 0, -1), (4, 0, -1), (5, 3, -2), (6, NONE, -1), (6, ODD, -1), (7, 192, -1), (7, 201, -1),
-              (8, NONE, -1), (2, 1 << 23, -2)])
+              (8, NONE, -1), (2, 1 << 23, -2), (3, (1 << 31) - 1, -2), (4, (1 << 31) - 1, -2)])
     assert lib.moe_quantize_weights_fp8(P, 200, 0, 50, 200, 0, P, 208, P, NONE) == 0
 
 
