@@ -14,6 +14,16 @@
 // A workgroup has a CU for itself, so nothing else runs while a tile begins or ends: the last D steps of a tile therefore load the first
 // D of the workgroup's next one.  Step j of it goes where step j of any tile is expected, stage j % D, which is free in that of the
 // last steps that has the same remainder.
+//
+// Products are e4m3 ones (v_mfma_f32_16x16x128_f8f6f4): inside a block they are aligned to the largest and what is more than 13 binary
+// places below it is dropped, sums of 128 normal values off by 1.5e-5 rms; a result in bf16 is off by 2^-9 = 2e-3.  Blocks are added in
+// fp32.  The e4m3 activation of the FFN moves over a border somewhat more often for it (error of y 2.0e-3 instead of 1.7e-3 rms).
+//
+// Measured on 16384 rows x 4096 columns in one group: 1.86 PFLOP/s at K = 4096, 2.10 at 7168, about 0.85 us a step of one tile.  Of that the
+// matrix instructions take 0.5 us; a step without its loads takes 0.73, without its scaled additions too 0.58, loads and barriers alone
+// 0.75: it is bound by two stages (96 KB) in flight and by issue, not by one unit.  Steps that brought it there, us: scales through LDS
+// instead of registers (16 lines a load, 8 waves) and loads between the products 437 -> 329; the next tile's loads, 365 -> 350 and results in
+// whole lines with products added two later 350 -> 332 (16 groups).  No difference: the order of tiles in bands of 4, 8 or 16.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
