@@ -45,15 +45,15 @@ __global__ __launch_bounds__(kFp8Threads, 2) void fp8_narrow_kernel(Fp8Args a, i
 
 // A workgroup per CU; each takes every n-th item of its XCD's list, big ones first.
 constexpr int kRingGrid = 256;
-template <bool kGateUp, typename OT>
+template <bool kGateUp, typename OT, bool kExact>
 __global__ __launch_bounds__(kRingThreads, 2) void fp8_ring_kernel(RingArgs a) {
     RingList list;
     int n[2];
-    list.read(a.group_offsets, a.groups, a.T * a.k, blockIdx.x & 7, a.ntn, n);
+    list.read(a.group_offsets, a.groups, a.T * a.k, blockIdx.x & 7, a.ntn, kExact, n);
     const int step = gridDim.x >> 3, id = blockIdx.x >> 3;
-    fp8_ring_items<kGateUp, OT, 0>(a, list, id, n[0], step);
+    fp8_ring_items<kGateUp, OT, 0, kExact>(a, list, id, n[0], step);
     __syncthreads();                                                 // the other class has other places in LDS
-    fp8_ring_items<kGateUp, OT, 1>(a, list, (id + step - n[0] % step) % step, n[1], step);       // in turn behind them
+    fp8_ring_items<kGateUp, OT, 1, kExact>(a, list, (id + step - n[0] % step) % step, n[1], step);       // in turn behind them
 }
 
 inline int launched() { return hipGetLastError() == hipSuccess ? METRO_OK : METRO_ERR_HIP; }
@@ -83,7 +83,7 @@ bool ring_fits(const Fp8Args& a, bool gate_up) {
     return a.K % kBlock == 0 && a.n_out % kBlock == 0 && rows * a.ldx < (1ull << 32) && (uint64_t)a.n_out * (gate_up ? 2 : 1) * a.ldw < (1ull << 32);
 }
 
-template <bool kGateUp, typename OT>
+template <bool kGateUp, typename OT, bool kExact>
 int launch_ring(RingArgs a, hipStream_t st) {
     const int cols = kGateUp ? 128 : 256;
     a.ntn = (a.n_out + cols - 1) / cols;
@@ -91,7 +91,7 @@ int launch_ring(RingArgs a, hipStream_t st) {
     const int64_t tiles = std::min<int64_t>(cap, max_tiles(cap, a.groups, kRingTileRows));
     const int64_t per_xcd = a.ntn < 8 ? (tiles * a.ntn + 7) / 8 : tiles * ((a.ntn + 7) / 8);
     const uint32_t grid = (uint32_t)std::min<int64_t>(8 * per_xcd, kRingGrid);
-    hipLaunchKernelGGL((fp8_ring_kernel<kGateUp, OT>), dim3(grid), dim3(kRingThreads), 0, st, a);
+    hipLaunchKernelGGL((fp8_ring_kernel<kGateUp, OT, kExact>), dim3(grid), dim3(kRingThreads), 0, st, a);
     return launched();
 }
 
@@ -103,9 +103,11 @@ constexpr int kRingPairs = 4096;
 // be resident.  Measured, K-split / ring tiles, us: one group of 4096 x 4096, 256 rows 18 / 27, 512 rows 32 / 28; of 2048 x 7168, 512 and 1024
 // rows 28 / 44 and 50 / 44; of 512 x 1024, 2048 rows 7.8 / 11.9; 16 groups of 2048 x 1024, 512 and 1024 rows 9.1 / 10.3 and 13.5 / 11.8; 32
 // groups of 4096 x 4096, 1024 and 2048 rows 107 / 128 and 157 / 135.
-bool many_rows(const Fp8Args& a) {
-    const int64_t cap = (int64_t)a.T * a.k;
-    return a.perm_pair ? cap > kRingPairs : cap > kNarrowRows32 * a.groups && cap * a.n_out >= (1 << 21);
+// fp32 results take the ring tiles with widened values, 64 rows at a time, which pay from four times as many rows on: one group of 4096 x
+// 4096, 1024 and 2048 rows 63 / 74 and 117 / 92; 16 groups, 2048 and 16384 rows 152 / 124 and 955 / 655.
+bool many_rows(const Fp8Args& a, int dtype) {
+    const int64_t cap = (int64_t)a.T * a.k, times = dtype == METRO_DTYPE_F32 ? 4 : 1;
+    return a.perm_pair ? cap > kRingPairs * times : cap > kNarrowRows32 * a.groups && cap * a.n_out >= times << 21;
 }
 
 constexpr int kMaxSide = 1 << 20;           // K, columns
@@ -141,10 +143,11 @@ extern "C" int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const
     if (T == 0) return METRO_OK;
     if (check_matrix(x, ldx, K, xs) != METRO_OK || check_matrix(w, ldw, K, ws) != METRO_OK || !y || misaligned(y)) return METRO_ERR_INVALID_ARG;
     const Fp8Args a{x, xs, perm_pair, group_offsets, (const uint8_t*)w, ws, y, ldx, T, k, groups, K, N, ldw, N, 0};
-    if (many_rows(a) && dtype == METRO_DTYPE_BF16 && ring_fits(a, false)) {
+    if (many_rows(a, dtype) && ring_fits(a, false)) {
         RingArgs r{};
         (Fp8Args&)r = a;
-        return launch_ring<false, __bf16>(r, (hipStream_t)stream);
+        return dtype == METRO_DTYPE_BF16 ? launch_ring<false, __bf16, false>(r, (hipStream_t)stream)
+                                         : launch_ring<false, float, true>(r, (hipStream_t)stream);
     }
     return launch<false, false>(a, dtype, (hipStream_t)stream);
 }
@@ -176,8 +179,8 @@ extern "C" int moe_grouped_ffn_fp8(const void* x, int ldx, const float* xs, cons
         up.act = act, up.act_scale = act_scale;
         (Fp8Args&)down = Fp8Args{act, act_scale, nullptr, group_offsets, (const uint8_t*)w2, s2, y_perm, I, T, k, spr, I, H, ldw2, H, 0};
         if (ring_fits(up, true) && ring_fits(down, false)) {
-            rc = launch_ring<true, float>(up, (hipStream_t)stream);
-            return rc != METRO_OK ? rc : launch_ring<false, __bf16>(down, (hipStream_t)stream);
+            rc = launch_ring<true, float, false>(up, (hipStream_t)stream);
+            return rc != METRO_OK ? rc : launch_ring<false, __bf16, false>(down, (hipStream_t)stream);
         }
     }
     const Fp8Args up{x, xs, perm_pair, group_offsets, (const uint8_t*)w13, s13, ws, ldx, T, k, spr, H, I, ldw13, ld_act, 0};

@@ -15,7 +15,8 @@
 // D of the workgroup's next one.  Step j of it goes where step j of any tile is expected, stage j % D, which is free in that of the
 // last steps that has the same remainder.
 //
-// Products are e4m3 ones (v_mfma_f32_16x16x128_f8f6f4): inside a block they are aligned to the largest and what is more than 13 binary
+// kExact (fp32 results, at most 64 rows a tile: more spill registers): values widened to bf16 as in fp8_split.h.  Otherwise
+// products are e4m3 ones (v_mfma_f32_16x16x128_f8f6f4): inside a block they are aligned to the largest and what is more than 13 binary
 // places below it is dropped, sums of 128 normal values off by 1.5e-5 rms; a result in bf16 is off by 2^-9 = 2e-3.  Blocks are added in
 // fp32.  The e4m3 activation of the FFN moves over a border somewhat more often for it (error of y 2.0e-3 instead of 1.7e-3 rms).
 //
@@ -121,7 +122,7 @@ struct RingSource {
 };
 
 // ready: the first D stages are in LDS or on their way.  has_next: the last steps load those of `then`.
-template <bool kGateUp, typename OT, int MT, typename Source>
+template <bool kGateUp, typename OT, int MT, bool kExact, typename Source>
 __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, const Source& now, const Source& then, bool ready, bool has_next) {
     constexpr bool kBig = MT > 2;
     constexpr int M2 = MT / 2, D = kBig ? 3 : 4, kXUnits = kBig ? 2 : 1;
@@ -187,7 +188,15 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, c
     };
     auto multiply = [&](auto I, float scale) {
         constexpr int i = decltype(I)::value, slot = i % kLate;
-        const floatx4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i / M2], fx[i % M2], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+        floatx4 p = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (kExact) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_e4m3(fw[i / M2][2 * c], fw[i / M2][2 * c + 1]),
+                                                            widen_e4m3(fx[i % M2][2 * c], fx[i % M2][2 * c + 1]), p, 0, 0, 0);
+        } else {
+            p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i / M2], fx[i % M2], p, 0, 0, 0, 0, 0, 0);
+        }
         add_late(std::integral_constant<int, i - kLate>{});
         late[slot] = p;
         late_scale[slot] = scale;
@@ -313,10 +322,16 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, c
             const int col = col0 + tx * 64 + q * 16;
             if (col >= a.n_out) continue;
             OT* out = reinterpret_cast<OT*>(a.dst) + (size_t)(t.row0 + row) * a.ldd + col;
+            if constexpr (sizeof(OT) == 4) {
 #pragma unroll
-            for (int b = 0; b < 4; b += 2)
-                *reinterpret_cast<u32x4*>(out + b * 4) = u32x4{pack_bf16x2(acc[b][mt][0], acc[b][mt][1]), pack_bf16x2(acc[b][mt][2], acc[b][mt][3]),
-                                                               pack_bf16x2(acc[b + 1][mt][0], acc[b + 1][mt][1]), pack_bf16x2(acc[b + 1][mt][2], acc[b + 1][mt][3])};
+                for (int b = 0; b < 4; ++b) *reinterpret_cast<floatx4*>(out + b * 4) = acc[b][mt];
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; b += 2)
+                    *reinterpret_cast<u32x4*>(out + b * 4) =
+                        u32x4{pack_bf16x2(acc[b][mt][0], acc[b][mt][1]), pack_bf16x2(acc[b][mt][2], acc[b][mt][3]),
+                              pack_bf16x2(acc[b + 1][mt][0], acc[b + 1][mt][1]), pack_bf16x2(acc[b + 1][mt][2], acc[b + 1][mt][3])};
+            }
         }
     }
 }
@@ -330,7 +345,7 @@ struct RingList {
     int begin, rows, first, stride, xcd, size;     // size: rows of a tile
     int tiles[2], incl[2];                      // of big ones, small ones: tiles of the slot, items of the slots up to it
 
-    __device__ __forceinline__ void read(const int32_t* __restrict__ group_offsets, int groups, int cap, int xcd_, int n_cols, int (&n)[2]) {
+    __device__ __forceinline__ void read(const int32_t* __restrict__ group_offsets, int groups, int cap, int xcd_, int n_cols, bool narrow, int (&n)[2]) {
         const int l = lane_id();
         int m = 0;
         begin = 0;
@@ -348,7 +363,7 @@ struct RingList {
             const int n = __builtin_amdgcn_readlane(wave_inclusive_sum((m + r - 1) / r), kWave - 1);
             return (int)(((int64_t)n * n_cols + gridDim.x - 1) / gridDim.x);
         };
-        size = 3 * (int64_t)rounds(kRingTileRows / 2) < 4 * (int64_t)rounds(kRingTileRows) ? kRingTileRows / 2 : kRingTileRows;
+        size = narrow || 3 * (int64_t)rounds(kRingTileRows / 2) < 4 * (int64_t)rounds(kRingTileRows) ? kRingTileRows / 2 : kRingTileRows;
         const int part = m & (size - 1), full = m / size;
         tiles[0] = full + (part > kSmallRows);
         tiles[1] = part > 0 && part <= kSmallRows;
@@ -379,7 +394,7 @@ struct RingList {
 };
 
 // The items id, id + step, ... of a class.
-template <bool kGateUp, typename OT, int kClass>
+template <bool kGateUp, typename OT, int kClass, bool kExact>
 __device__ __forceinline__ void fp8_ring_items(const RingArgs& a, const RingList& list, int id, int n, int step) {
     using Source = RingSource<kGateUp, kClass ? 1 : 2>;
     if (id >= n) return;
@@ -393,9 +408,9 @@ __device__ __forceinline__ void fp8_ring_items(const RingArgs& a, const RingList
         then.set(a, t1, raw, wv);
         const Tile t2 = id + 2 * step < n ? list.tile<kClass>(id + 2 * step) : t1;
         raw = Source::raw(a, t2);
-        if constexpr (kClass == 1) fp8_ring_tile<kGateUp, OT, 2>(a, t, now, then, ready, more);
-        else if (t.rows <= 64) fp8_ring_tile<kGateUp, OT, 4>(a, t, now, then, ready, more);
-        else fp8_ring_tile<kGateUp, OT, 8>(a, t, now, then, ready, more);
+        if constexpr (kClass == 1) fp8_ring_tile<kGateUp, OT, 2, kExact>(a, t, now, then, ready, more);
+        else if (kExact || t.rows <= 64) fp8_ring_tile<kGateUp, OT, 4, kExact>(a, t, now, then, ready, more);
+        else if constexpr (!kExact) fp8_ring_tile<kGateUp, OT, 8, false>(a, t, now, then, ready, more);
         if (!more) return;
         id += step;
         t = t1, t1 = t2;

@@ -189,6 +189,8 @@ def many(sizes, N):
     ([300, 0, 1, 513], 896, 384), ([40], 1024, 2176), ([200], 2048, 256), ([1100, 1000], 128, 256), ([20] * 64, 1152, 128)])
 def test_product_of_many_rows(sizes, K, N):
     run_mm(sizes, K, N, "bf16", rows=many(sizes, N), product=ref.product_many)
+    if N >= 384:                                                    # fp32 results: from four times as many on
+        run_mm(sizes, K, N, "f32", rows=4 * many(sizes, N))
 
 
 @pytest.mark.parametrize("K", [128, 256, 384, 512, 640, 1152])
@@ -197,6 +199,7 @@ def test_product_of_more_tiles_than_workgroups(K):
     tiles of both kinds and small ones, a change from the ones to the others, fewer columns than XCDs and more."""
     run_mm([7000, 1500, 70, 1, 20, 45, 8, 300], K, 1024, "bf16", product=ref.product_many)
     run_mm([2900, 40, 1, 129, 31], K, 2304, "bf16", product=ref.product_many)
+    run_mm([2900, 40, 1, 129, 31], K, 2304, "f32", rows=3700)
     run_mm([20, 3, 31, 0] * 16, K, 2176, "bf16", rows=many([20, 3, 31, 0] * 16, 2176), product=ref.product_many)
 
 
