@@ -1,13 +1,13 @@
 // moe_grouped_mm_fp8 and moe_grouped_ffn_fp8: rows sorted by expert times their expert's e4m3 weights, rows and weights with an fp32
 // scale for each block of 128 (fp8_common.h).
 //
+// Values are widened to bf16, so products are exact and sums fp32 in both forms; a result depends on the form by the order of its sums only.
 // Few rows a group (fp8_split.h): bound by the weights' bytes, half of bf16's, every activated weight row streamed once per tile of at most
-// 32 rows; values are widened to bf16, so sums are fp32.  The FFN's activation between the products stays fp32 in memory and is quantized by
-// the tiles that read it, which saves a launch.
-// Many rows a group (fp8_ring.h): tiles of 128 rows x 256 weight rows, e4m3 products, the activation quantized where it is made.
+// 32 rows.  The FFN's activation between the products stays fp32 in memory and is quantized by the tiles that read it, which saves a launch.
+// Many rows a group (fp8_ring.h): tiles of 128 or 64 rows x 256 weight rows, the activation quantized where it is made.
 // Measured, us: FFN, a rank of eight, 8 tokens at 2048 x 768 13.2 (kernels of 7.0 + 5.2; the weights alone 3.8 at 6.2 TB/s), 97 tokens at 7168 x
-// 2048 193 (5.9 TB/s of weights), 1024 tokens 324 (bf16 experts: 606), 4000 tokens at 2048 x 768 50; product of 16384 rows in 16 groups,
-// 4096 x 4096, 332 (1.65 PFLOP/s under sustained load).
+// 2048 193 (5.9 TB/s of weights), 1024 tokens 360 (bf16 experts: 606), 4000 tokens at 2048 x 768 63; product of 16384 rows in 16 groups,
+// 4096 x 4096, 527 (1.04 PFLOP/s under sustained load).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -45,15 +45,15 @@ __global__ __launch_bounds__(kFp8Threads, 2) void fp8_narrow_kernel(Fp8Args a, i
 
 // A workgroup per CU; each takes every n-th item of its XCD's list, big ones first.
 constexpr int kRingGrid = 256;
-template <bool kGateUp, typename OT, bool kExact>
+template <bool kGateUp, typename OT>
 __global__ __launch_bounds__(kRingThreads, 2) void fp8_ring_kernel(RingArgs a) {
     RingList list;
     int n[2];
-    list.read(a.group_offsets, a.groups, a.T * a.k, blockIdx.x & 7, a.ntn, kExact, n);
+    list.read(a.group_offsets, a.groups, a.T * a.k, blockIdx.x & 7, a.ntn, n);
     const int step = gridDim.x >> 3, id = blockIdx.x >> 3;
-    fp8_ring_items<kGateUp, OT, 0, kExact>(a, list, id, n[0], step);
+    fp8_ring_items<kGateUp, OT, 0>(a, list, id, n[0], step);
     __syncthreads();                                                 // the other class has other places in LDS
-    fp8_ring_items<kGateUp, OT, 1, kExact>(a, list, (id + step - n[0] % step) % step, n[1], step);       // in turn behind them
+    fp8_ring_items<kGateUp, OT, 1>(a, list, (id + step - n[0] % step) % step, n[1], step);       // in turn behind them
 }
 
 inline int launched() { return hipGetLastError() == hipSuccess ? METRO_OK : METRO_ERR_HIP; }
@@ -83,7 +83,7 @@ bool ring_fits(const Fp8Args& a, bool gate_up) {
     return a.K % kBlock == 0 && a.n_out % kBlock == 0 && rows * a.ldx < (1ull << 32) && (uint64_t)a.n_out * (gate_up ? 2 : 1) * a.ldw < (1ull << 32);
 }
 
-template <bool kGateUp, typename OT, bool kExact>
+template <bool kGateUp, typename OT>
 int launch_ring(RingArgs a, hipStream_t st) {
     const int cols = kGateUp ? 128 : 256;
     a.ntn = (a.n_out + cols - 1) / cols;
@@ -91,23 +91,24 @@ int launch_ring(RingArgs a, hipStream_t st) {
     const int64_t tiles = std::min<int64_t>(cap, max_tiles(cap, a.groups, kRingTileRows));
     const int64_t per_xcd = a.ntn < 8 ? (tiles * a.ntn + 7) / 8 : tiles * ((a.ntn + 7) / 8);
     const uint32_t grid = (uint32_t)std::min<int64_t>(8 * per_xcd, kRingGrid);
-    hipLaunchKernelGGL((fp8_ring_kernel<kGateUp, OT, kExact>), dim3(grid), dim3(kRingThreads), 0, st, a);
+    hipLaunchKernelGGL((fp8_ring_kernel<kGateUp, OT>), dim3(grid), dim3(kRingThreads), 0, st, a);
     return launched();
 }
 
 // Ring tiles for batches of many rows.  With token lists the host knows T * k, of which a rank of eight has an eighth: more than 4096.
-// Measured, the FFN of such a rank, K-split / ring tiles, us: 512 tokens (k = 8) 35 / 36 at 2048 x 768, 103 / 100 at 4096 x 1536, 299 / 310 at
-// 7168 x 2048; 256 tokens 29 / 34, 84 / 88, 272 / 293; 768 and 640 tokens 43 / 39, 104 / 93, 321 / 318 (1024 of the last: 466 / 326).
+// Measured, the FFN of such a rank, K-split / ring tiles, us: 512 tokens (k = 8) 36 / 40 at 2048 x 768, 105 / 98 at 4096 x 1536, 298 / 319 at
+// 7168 x 2048; 256 tokens 30 / 39, 85 / 89, 270 / 295; 768, 640 and 640 tokens 43 / 40, 104 / 102, 320 / 320 (1024 of the last: 462 / 365).
 constexpr int kRingPairs = 4096;
-// Rows in order are all there.  More than one K-split tile a group, and at least 1024 items of these, two for every workgroup that can
-// be resident.  Measured, K-split / ring tiles, us: one group of 4096 x 4096, 256 rows 18 / 27, 512 rows 32 / 28; of 2048 x 7168, 512 and 1024
-// rows 28 / 44 and 50 / 44; of 512 x 1024, 2048 rows 7.8 / 11.9; 16 groups of 2048 x 1024, 512 and 1024 rows 9.1 / 10.3 and 13.5 / 11.8; 32
-// groups of 4096 x 4096, 1024 and 2048 rows 107 / 128 and 157 / 135.
-// fp32 results take the ring tiles with widened values, 64 rows at a time, which pay from four times as many rows on: one group of 4096 x
-// 4096, 1024 and 2048 rows 63 / 74 and 117 / 92; 16 groups, 2048 and 16384 rows 152 / 124 and 955 / 655.
-bool many_rows(const Fp8Args& a, int dtype) {
-    const int64_t cap = (int64_t)a.T * a.k, times = dtype == METRO_DTYPE_F32 ? 4 : 1;
-    return a.perm_pair ? cap > kRingPairs * times : cap > kNarrowRows32 * a.groups && cap * a.n_out >= times << 21;
+// Rows in order are all there.  More than one K-split tile a group, and 2048 items of these, four for every workgroup that can be
+// resident.  Measured, K-split / ring tiles, us, bf16: one group of 4096 x 4096, 512, 1024 and 2048 rows 32 / 56, 59 / 58 and 110 / 69; of
+// 2048 x 7168, 1024 rows 52 / 90; of 512 x 1024, 4096 rows 15 / 20; 4 groups of 4096 x 4096, 512 and 1024 rows 35 / 55 and 61 / 58; 16
+// groups, 1024, 2048 and 16384 rows 92 / 71, 149 / 117 and 938 / 541; 16 groups of 2048 x 1024, 1024 and 2048 rows 17.0 / 16.6 and 26.8 /
+// 23.1; 32 groups of 4096 x 4096, 1024 and 2048 rows 122 / 110 and 180 / 143.  fp32: one group of 4096 x 4096, 512, 1024 and 2048 rows
+// 33 / 58, 60 / 63 and 113 / 77; 16 groups, 1024 and 2048 rows 92 / 75 and 152 / 128.
+constexpr int64_t kRingProducts = 1 << 22;  // rows x columns
+bool many_rows(const Fp8Args& a) {
+    const int64_t cap = (int64_t)a.T * a.k;
+    return a.perm_pair ? cap > kRingPairs : cap > kNarrowRows32 * a.groups && cap * a.n_out >= kRingProducts;
 }
 
 constexpr int kMaxSide = 1 << 20;           // K, columns
@@ -143,11 +144,11 @@ extern "C" int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const
     if (T == 0) return METRO_OK;
     if (check_matrix(x, ldx, K, xs) != METRO_OK || check_matrix(w, ldw, K, ws) != METRO_OK || !y || misaligned(y)) return METRO_ERR_INVALID_ARG;
     const Fp8Args a{x, xs, perm_pair, group_offsets, (const uint8_t*)w, ws, y, ldx, T, k, groups, K, N, ldw, N, 0};
-    if (many_rows(a, dtype) && ring_fits(a, false)) {
+    if (many_rows(a) && ring_fits(a, false)) {
         RingArgs r{};
         (Fp8Args&)r = a;
-        return dtype == METRO_DTYPE_BF16 ? launch_ring<false, __bf16, false>(r, (hipStream_t)stream)
-                                         : launch_ring<false, float, true>(r, (hipStream_t)stream);
+        return dtype == METRO_DTYPE_BF16 ? launch_ring<false, __bf16>(r, (hipStream_t)stream)
+                                         : launch_ring<false, float>(r, (hipStream_t)stream);
     }
     return launch<false, false>(a, dtype, (hipStream_t)stream);
 }
@@ -179,8 +180,8 @@ extern "C" int moe_grouped_ffn_fp8(const void* x, int ldx, const float* xs, cons
         up.act = act, up.act_scale = act_scale;
         (Fp8Args&)down = Fp8Args{act, act_scale, nullptr, group_offsets, (const uint8_t*)w2, s2, y_perm, I, T, k, spr, I, H, ldw2, H, 0};
         if (ring_fits(up, true) && ring_fits(down, false)) {
-            rc = launch_ring<true, float, false>(up, (hipStream_t)stream);
-            return rc != METRO_OK ? rc : launch_ring<false, __bf16, false>(down, (hipStream_t)stream);
+            rc = launch_ring<true, float>(up, (hipStream_t)stream);
+            return rc != METRO_OK ? rc : launch_ring<false, __bf16>(down, (hipStream_t)stream);
         }
     }
     const Fp8Args up{x, xs, perm_pair, group_offsets, (const uint8_t*)w13, s13, ws, ldx, T, k, spr, H, I, ldw13, ld_act, 0};

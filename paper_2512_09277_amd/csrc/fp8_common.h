@@ -16,8 +16,6 @@ constexpr int kBlock = 128;                 // values of a row that share a scal
 constexpr float kE4m3Max = 448.f;
 constexpr float kSmallest = 1e-30f;
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
 struct BlockScale { float scale, inverse; };

@@ -15,16 +15,18 @@
 // D of the workgroup's next one.  Step j of it goes where step j of any tile is expected, stage j % D, which is free in that of the
 // last steps that has the same remainder.
 //
-// kExact (fp32 results, at most 64 rows a tile: more spill registers): values widened to bf16 as in fp8_split.h.  Otherwise
-// products are e4m3 ones (v_mfma_f32_16x16x128_f8f6f4): inside a block they are aligned to the largest and what is more than 13 binary
-// places below it is dropped, sums of 128 normal values off by 1.5e-5 rms; a result in bf16 is off by 2^-9 = 2e-3.  Blocks are added in
-// fp32.  The e4m3 activation of the FFN moves over a border somewhat more often for it (error of y 2.0e-3 instead of 1.7e-3 rms).
+// The values are widened to bf16 as in fp8_split.h: products are exact, sums fp32.  The matrix cores' own e4m3 products
+// (v_mfma_f32_16x16x128_f8f6f4) are faster, 337 us for 16384 rows x 4096 x 4096 in 16 groups instead of 530, but they align the products of
+// a block to the largest and drop what is more than 13 binary places below it: of 448 * 448 - 448 * 448 + 126 nothing is left.
 //
-// Measured on 16384 rows x 4096 columns in one group: 1.86 PFLOP/s at K = 4096, 2.10 at 7168, about 0.85 us a step of one tile.  Of that the
-// matrix instructions take 0.5 us; a step without its loads takes 0.73, without its scaled additions too 0.58, loads and barriers alone
-// 0.75: it is bound by two stages (96 KB) in flight and by issue, not by one unit.  Steps that brought it there, us: scales through LDS
-// instead of registers (16 lines a load, 8 waves) and loads between the products 437 -> 329; the next tile's loads, 365 -> 350 and results in
-// whole lines with products added two later 350 -> 332 (16 groups).  No difference: the order of tiles in bands of 4, 8 or 16.
+// A step's activations are widened once, in front, and 16 weight rows at a time once per step and wave: 128 conversions for 64 products.
+//
+// Measured on 16384 rows x 4096 columns in one group: 1.08 PFLOP/s at K = 4096, 1.17 at 7168, 1.84 us a step of a tile of 128 rows.  Vector
+// instructions bound it: 277 of a wave and step (the conversions 4.5 cycles each, the scaled additions, addresses) beside 64 matrix
+// instructions of 17.6 cycles, two waves to a SIMD.
+// Before that, with e4m3 products: scales through LDS instead of registers (16 lines a load, 8 waves) and loads between the products
+// 437 -> 329 us; the next tile's loads 365 -> 350 and results in whole lines with products added two later 350 -> 332 (16 groups).  No
+// difference: the order of tiles in bands of 4, 8 or 16; now, the matrix instructions of two products in turn.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -122,7 +124,7 @@ struct RingSource {
 };
 
 // ready: the first D stages are in LDS or on their way.  has_next: the last steps load those of `then`.
-template <bool kGateUp, typename OT, int MT, bool kExact, typename Source>
+template <bool kGateUp, typename OT, int MT, typename Source>
 __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, const Source& now, const Source& then, bool ready, bool has_next) {
     constexpr bool kBig = MT > 2;
     constexpr int M2 = MT / 2, D = kBig ? 3 : 4, kXUnits = kBig ? 2 : 1;
@@ -159,14 +161,14 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, c
         __builtin_amdgcn_raw_ptr_buffer_load_lds(f.scale, (__attribute__((address_space(3))) void*)(ring_scale<set>() + s_at), 4,
                                                  (int)(f.own ? now.s_lane : then.s_lane), f.at * 4, 0, 0);
     };
-    const int rd = r16 * 128 + ((q ^ (r16 & 7)) * 16);
-    i32x8 fw[4], fx[M2];                                    // each is replaced once it has been multiplied
-    auto fragment = [&](const char* p) {
-        const u32x4 lo = *reinterpret_cast<const u32x4*>(p + rd), hi = *reinterpret_cast<const u32x4*>(p + (rd ^ 64));
-        i32x8 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (int)lo[e], v[4 + e] = (int)hi[e];
-        return v;
+    int rd = r16 * 128 + ((q ^ (r16 & 7)) * 16);
+    struct Bytes { u32x4 lo, hi; };
+    struct Wide { bf16x8 part[4]; };
+    Bytes fw[4], fx[M2];                                    // of the next step once they have been widened
+    Wide xw[M2];
+    auto fragment = [&](const char* p) { return Bytes{*reinterpret_cast<const u32x4*>(p + rd), *reinterpret_cast<const u32x4*>(p + (rd ^ 64))}; };
+    auto widen = [](const Bytes& f) {
+        return Wide{{widen_e4m3(f.lo[0], f.lo[1]), widen_e4m3(f.lo[2], f.lo[3]), widen_e4m3(f.hi[0], f.hi[1]), widen_e4m3(f.hi[2], f.hi[3])}};
     };
     auto read_w = [&](auto U, auto B) {
         constexpr int set = decltype(U)::value % D, b = decltype(B)::value;
@@ -186,17 +188,11 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, c
 #pragma unroll
         for (int v = 0; v < 4; ++v) acc[i / M2][i % M2][v] = fmaf(late[slot][v], late_scale[slot], acc[i / M2][i % M2][v]);
     };
-    auto multiply = [&](auto I, float scale) {
+    auto multiply = [&](auto I, const Wide& w, const Wide& x, float scale) {
         constexpr int i = decltype(I)::value, slot = i % kLate;
         floatx4 p = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (kExact) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_e4m3(fw[i / M2][2 * c], fw[i / M2][2 * c + 1]),
-                                                            widen_e4m3(fx[i % M2][2 * c], fx[i % M2][2 * c + 1]), p, 0, 0, 0);
-        } else {
-            p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i / M2], fx[i % M2], p, 0, 0, 0, 0, 0, 0);
-        }
+        for (int c = 0; c < 4; ++c) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.part[c], x.part[c], p, 0, 0, 0);
         add_late(std::integral_constant<int, i - kLate>{});
         late[slot] = p;
         late_scale[slot] = scale;
@@ -228,14 +224,18 @@ __device__ __forceinline__ void fp8_ring_tile(const RingArgs& a, const Tile t, c
             if constexpr (kGateUp) scale[1][mt] = xscale[mt] * wscale[1];
         }
         const From f = from(s + D, u % D);
+        asm volatile("" : "+v"(rd));                        // or the addresses of all units, computed ahead, spill registers
+#pragma unroll
+        for (int mt = 0; mt < M2; ++mt) xw[mt] = widen(fx[mt]);
         arrive(std::integral_constant<int, (D - 2) * kLoads>{});
         read_scale(next);
         load_scale(U, f);
         run_steps(std::make_integer_sequence<int, 4>{}, [&](auto B, int) {
             constexpr int b = decltype(B)::value;
+            const Wide ww = widen(fw[b]);
             run_steps(std::make_integer_sequence<int, M2>{}, [&](auto M, int) {
                 constexpr int mt = decltype(M)::value, at = b * M2 + mt;
-                multiply(std::integral_constant<int, at>{}, scale[kGateUp ? b >> 1 : 0][mt]);
+                multiply(std::integral_constant<int, at>{}, ww, xw[mt], scale[kGateUp ? b >> 1 : 0][mt]);
                 if constexpr (b == 3) read_x(next, M);
                 constexpr int begin = at * kUnitLoads / (4 * M2), end = (at + 1) * kUnitLoads / (4 * M2);
                 if constexpr (end > begin) load(U, std::integral_constant<int, begin>{}, f);
@@ -345,7 +345,7 @@ struct RingList {
     int begin, rows, first, stride, xcd, size;     // size: rows of a tile
     int tiles[2], incl[2];                      // of big ones, small ones: tiles of the slot, items of the slots up to it
 
-    __device__ __forceinline__ void read(const int32_t* __restrict__ group_offsets, int groups, int cap, int xcd_, int n_cols, bool narrow, int (&n)[2]) {
+    __device__ __forceinline__ void read(const int32_t* __restrict__ group_offsets, int groups, int cap, int xcd_, int n_cols, int (&n)[2]) {
         const int l = lane_id();
         int m = 0;
         begin = 0;
@@ -355,15 +355,15 @@ struct RingList {
         }
         rows = m;
         xcd = xcd_;
-        // Rounds of the launch's workgroups with tiles of 128 and of 64 rows, of which one takes about three quarters of the time.
-        // Measured, the FFN, us, 128 rows always / by this rule: 640, 1024, 2048 and 4000 tokens at 2048 x 768 36.1 / 32.7, 38.5 / 35.0,
-        // 41.1 / 38.8, 52.5 / 50.3; 640 and 1024 at 4096 x 1536 92.7 / 93.6, 101.8 / 97.4; at 7168 x 2048 316.2 / 311.6, 325.3 / 328.9 (357 where
-        // two thirds are assumed).
+        // Rounds of the launch's workgroups with tiles of 128 and of 64 rows, of which one takes about three quarters of the time (0.59
+        // where the weights are not what it waits for).  Measured, the FFN, us, 128 rows always / by this rule: 640, 1024, 2048 and 4000 tokens
+        // at 2048 x 768 52.7 / 39.4, 53.2 / 41.0, 54.6 / 46.1, 64.4 / 65.2; 640 and 1024 at 4096 x 1536 105.5 / 101.8, 118.9 / 109.4; at
+        // 7168 x 2048 326.6 / 320.4, 358.2 / 364.8 (383.9 where two thirds are assumed).
         auto rounds = [&](int r) {
             const int n = __builtin_amdgcn_readlane(wave_inclusive_sum((m + r - 1) / r), kWave - 1);
             return (int)(((int64_t)n * n_cols + gridDim.x - 1) / gridDim.x);
         };
-        size = narrow || 3 * (int64_t)rounds(kRingTileRows / 2) < 4 * (int64_t)rounds(kRingTileRows) ? kRingTileRows / 2 : kRingTileRows;
+        size = 3 * (int64_t)rounds(kRingTileRows / 2) < 4 * (int64_t)rounds(kRingTileRows) ? kRingTileRows / 2 : kRingTileRows;
         const int part = m & (size - 1), full = m / size;
         tiles[0] = full + (part > kSmallRows);
         tiles[1] = part > 0 && part <= kSmallRows;
@@ -394,7 +394,7 @@ struct RingList {
 };
 
 // The items id, id + step, ... of a class.
-template <bool kGateUp, typename OT, int kClass, bool kExact>
+template <bool kGateUp, typename OT, int kClass>
 __device__ __forceinline__ void fp8_ring_items(const RingArgs& a, const RingList& list, int id, int n, int step) {
     using Source = RingSource<kGateUp, kClass ? 1 : 2>;
     if (id >= n) return;
@@ -408,9 +408,9 @@ __device__ __forceinline__ void fp8_ring_items(const RingArgs& a, const RingList
         then.set(a, t1, raw, wv);
         const Tile t2 = id + 2 * step < n ? list.tile<kClass>(id + 2 * step) : t1;
         raw = Source::raw(a, t2);
-        if constexpr (kClass == 1) fp8_ring_tile<kGateUp, OT, 2, kExact>(a, t, now, then, ready, more);
-        else if (kExact || t.rows <= 64) fp8_ring_tile<kGateUp, OT, 4, kExact>(a, t, now, then, ready, more);
-        else if constexpr (!kExact) fp8_ring_tile<kGateUp, OT, 8, false>(a, t, now, then, ready, more);
+        if constexpr (kClass == 1) fp8_ring_tile<kGateUp, OT, 2>(a, t, now, then, ready, more);
+        else if (t.rows <= 64) fp8_ring_tile<kGateUp, OT, 4>(a, t, now, then, ready, more);
+        else fp8_ring_tile<kGateUp, OT, 8>(a, t, now, then, ready, more);
         if (!more) return;
         id += step;
         t = t1, t1 = t2;
