@@ -29,7 +29,8 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// The kernels take whole vectors of a row, then the elements that are left.  kAny: rows that are no whole vectors, or not 16-byte aligned;
+// The kernels take whole vectors of a row, then the elements that are left, lane < H - n_vec * kN: with H next to 2^31 the sum
+// n_vec * kN + lane passes it.  kAny: rows that are no whole vectors, or not 16-byte aligned;
 // their vectors start anywhere (2048 tokens x 2001 in bf16, k = 6, all pairs here, us, against element by element: sort 12.7 -> 11.5,
 // its gradient 21.9 -> 11.8, gradient of the combine 63 -> 30).
 // Lanes of a token: a wave (kWaveToken), four tokens to a workgroup, or the workgroup.
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void permute_rows_kernel(const void* __re
                     if (c0 + u * kLanes < n_vec) V::store(x_perm, (size_t)row[j] * H + (c0 + u * kLanes) * kN, v[u]);
             }
         }
-        if (kAny && n_vec * kN + lane < H) {
+        if (kAny && lane < H - n_vec * kN) {
             const auto v = E::load(x, (size_t)t * H + n_vec * kN + lane);
 #pragma unroll
             for (int j = 0; j < kPairs; ++j)
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void unpermute_backward_kernel(const void
         };
         if (any) {
             for (int c = lane; c < n_vec; c += kLanes) columns(RowVec<kBf16, kN, kAny>{}, c * kN);
-            if (kAny && n_vec * kN + lane < H) columns(RowVec<kBf16, 1>{}, n_vec * kN + lane);
+            if (kAny && lane < H - n_vec * kN) columns(RowVec<kBf16, 1>{}, n_vec * kN + lane);
 #pragma unroll
             for (int j = 0; j < kPairs; ++j)
                 if (row[j] >= 0) dot[j] = wave_sum(dot[j]);
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void sum_rows_kernel(const void* __restri
         V::store(dx, (size_t)t * H + at, V::narrow(sum));
     };
     for (int c = lane; c < n_vec; c += kLanes) columns(RowVec<kBf16, kN, true>{}, c * kN);
-    if (n_vec * kN + lane < H) columns(RowVec<kBf16, 1>{}, n_vec * kN + lane);
+    if (lane < H - n_vec * kN) columns(RowVec<kBf16, 1>{}, n_vec * kN + lane);
 }
 
 // f(kBf16, kAny, kWaveToken, workgroups): a wave per token up to 2 vectors a lane.  Measured for the gradient of the combine, us, a
