@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void unpermute_scalar_kernel(const void* 
                                                                     void* __restrict__ out) {
     const int t = blockIdx.x;
     const int cap = (int)gridDim.x * k;
-    for (int c = threadIdx.x; c < H; c += kThreads) {
+    for (uint32_t c = threadIdx.x; c < (uint32_t)H; c += kThreads) {       // an int would pass 2^31 behind the longest rows
         float acc = 0.f;
         for (int j = 0; j < k; ++j) {
             const int r = pair_row[(size_t)t * k + j];

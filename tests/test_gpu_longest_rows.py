@@ -57,3 +57,17 @@ def test_gradient_of_the_combine(row):
     want = g[0, [0, H - 9, H - 7, H - 1]].double().sum()
     assert abs(dw.double() - want) <= 4 * 2.0 ** -24 * want
     assert torch.equal(dy, g * 0.5) and (memory[H:] == -7).all()
+
+
+def test_combine(row):
+    """Rows that are no whole vectors are combined element by element."""
+    import torch
+
+    from paper_2512_09277_amd import api
+
+    y, _ = row
+    here, half = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.full((1, 1), 0.5, device="cuda")
+    out, memory = guarded()
+    api.moe_unpermute(y, here, half, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, y * 0.5) and (memory[H:] == -7).all()
