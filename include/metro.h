@@ -244,8 +244,8 @@ int moe_unpermute_backward(const void* dout, const void* y_perm, const int32_t* 
  * 8-bit experts.  Values are OCP e4m3 (1 byte; largest 448), with one fp32 scale for each block of 128: a value stands for
  * byte * scale.  Activations have a scale for each 128 consecutive values of a row, scale [rows, ceil(K/128)]; a weight matrix one for
  * each 128 rows x 128 columns, scale [ceil(rows/128), ceil(K/128)].  The last block of a row or matrix may be short.
- * e4m3 rows are `ld` bytes apart, ld >= K, a multiple of 16 and at most 2^28, and start 16-byte aligned; the bytes from K up to the next multiple of
- * 16 are read (their values do not matter), so they must be there, behind the last row too.
+ * e4m3 rows are `ld` bytes apart, ld >= K, a multiple of 16 and, where a product reads them, at most 2^28, and start 16-byte aligned; a product
+ * reads the bytes from K up to the next multiple of 16 (their values do not matter), so they must be there, behind the last row too.
  *
  * moe_quantize_fp8 -- rows of activations (or of a gradient).  With m = max(largest magnitude of a block, 1e-30):
  *     scale = m / 448        q = the e4m3 value nearest to x * (448 / m), ties to even        (each operation rounded to fp32)
@@ -284,7 +284,8 @@ int moe_grouped_mm_fp8(const void* x, int ldx, const float* xs, const int32_t* p
                        int groups, int K, int N, const void* w, int ldw, const float* ws, int dtype, void* y, void* stream);
 
 /*
- * moe_grouped_ffn_fp8 -- moe_grouped_ffn on 8-bit experts.  For row r of local slot l, token t = perm_pair[r] / k:
+ * moe_grouped_ffn_fp8 -- moe_grouped_ffn on 8-bit experts, products and sums in fp32 as in moe_grouped_mm_fp8.  For row r of local slot l, token
+ * t = perm_pair[r] / k:
  *     gate, up = x[t] . w13[l]^T          (as in moe_grouped_mm_fp8 with perm_pair)
  *     act = silu(gate) * up in fp32, then to e4m3 with a scale for each 128 as by moe_quantize_fp8
  *     y_perm[r] = act . w2[l]^T

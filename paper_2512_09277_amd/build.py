@@ -18,7 +18,7 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared", "-fno
          "-Wall", "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option"]
 
 
-RESOURCES: dict = {}        # kernel symbol -> {"VGPRs": .., "AGPRs": .., "Occupancy": .., "LDS": .., "Scratch": ..} of the last build
+RESOURCES: dict = {}        # kernel symbol -> {"VGPRs": .., "AGPRs": .., "Occupancy": .., "LDS": .., "Scratch": .., "SGPRs Spill": ..} of the last build
 
 
 def call_flags(include: str = os.path.join(ROOT, "include")) -> list:
@@ -62,9 +62,9 @@ def build(verbose: bool = False, extra=()) -> str:
         m = re.search(r"Function Name: (\S+)", line)
         if m:
             name = m.group(1)
-        m = re.search(r"(VGPRs|AGPRs|Occupancy \[waves/SIMD\]|ScratchSize \[bytes/lane\]|LDS Size \[bytes/block\]): (\d+)", line)
+        m = re.search(r"(VGPRs|AGPRs|SGPRs Spill|Occupancy \[waves/SIMD\]|ScratchSize \[bytes/lane\]|LDS Size \[bytes/block\]): (\d+)", line)
         if m:
-            short = {"VGPRs": "VGPRs", "AGPRs": "AGPRs", "Occupancy [waves/SIMD]": "Occupancy",
+            short = {"VGPRs": "VGPRs", "AGPRs": "AGPRs", "SGPRs Spill": "SGPRs Spill", "Occupancy [waves/SIMD]": "Occupancy",
                      "ScratchSize [bytes/lane]": "Scratch", "LDS Size [bytes/block]": "LDS"}[m.group(1)]
             RESOURCES.setdefault(name, {})[short] = int(m.group(2))
             report.append((name, m.group(1), int(m.group(2))))
@@ -84,15 +84,16 @@ def build(verbose: bool = False, extra=()) -> str:
 
 def resources_markdown() -> str:
     """The compiler's per-kernel resource report of the last build() as a markdown table."""
-    rows = ["| kernel | VGPRs | AGPRs | static LDS bytes | scratch | occupancy (waves/SIMD, compiler) |", "|---|---|---|---|---|---|"]
-    demangle = subprocess.run(["c++filt"], input="\n".join(RESOURCES), stdout=subprocess.PIPE, text=True).stdout.splitlines()
+    rows = ["| kernel | VGPRs | AGPRs | static LDS bytes | scratch | SGPRs spilled to VGPRs | occupancy (waves/SIMD, compiler) |",
+            "|---|---|---|---|---|---|---|"]
+    # the mangled name of __bf16, which c++filt does not know, as that of a vendor's type
+    demangle = subprocess.run(["c++filt"], input="\n".join(RESOURCES).replace("DF16b", "u6__bf16"), stdout=subprocess.PIPE,
+                              text=True).stdout.splitlines()
     for sym, pretty in zip(RESOURCES, demangle):
         r = RESOURCES[sym]
-        pretty = pretty.replace("metro::(anonymous namespace)::", "").replace("void ", "").split("(")[0]
-        m = re.match(r"_ZN5metro12_GLOBAL__N_1\d+([a-z_]+)I", pretty)      # __bf16 instantiations are not demangled
-        if m:
-            pretty = m.group(1) + "<__bf16>"
-        rows.append(f"| {pretty} | {r.get('VGPRs')} | {r.get('AGPRs')} | {r.get('LDS')} | {r.get('Scratch')} | {r.get('Occupancy')} |")
+        pretty = pretty.replace("metro::(anonymous namespace)::", "").replace("void ", "").rsplit("(", 1)[0]
+        rows.append(f"| {pretty} | {r.get('VGPRs')} | {r.get('AGPRs')} | {r.get('LDS')} | {r.get('Scratch')} | {r.get('SGPRs Spill')} | "
+                    f"{r.get('Occupancy')} |")
     return "\n".join(rows)
 
 
